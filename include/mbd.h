@@ -424,6 +424,86 @@ MBD_API mbd_status mbd_block_reduce(const float* parts_dev, int S, int64_t M, in
 MBD_API mbd_status mbd_softmax_xent(const float* logits_dev, int64_t B, int64_t d, const int32_t* labels_dev,
                             void* dY_dev, int dY_bf16, float* per_sample_dev, int sync, void* cuda_stream);
 
+/* ---- Products grouped by expert ----
+ * A layer whose rows belong to E experts, each with a weight matrix of its own: the three contractions of Section 1 on ragged
+ * groups of rows.  The rows of a batch lie sorted by expert; group e is the rows offsets_dev[e] <= r < offsets_dev[e + 1]
+ * (E + 1 int32 on the DEVICE: the call never waits to learn them).
+ *   variant 0 (forward)          Y[r, :]  = X[r, :]  W_e^T (+ bias_e), ReLU    A = X [T, d_in],   B = W [E][d_out, d_in], out = Y [T, d_out]
+ *   variant 1 (backward-data)    dX[r, :] = dY[r, :] W_e, masked               A = dY [T, d_out], B = W [E][d_out, d_in], out = dX [T, d_in]
+ *   variant 2 (backward-weight)  dW_e     = sum over the group dY_r^T X_r      A = dY [T, d_out], B = X [T, d_in],        out = dW [E][d_out, d_in]
+ * bf16 operands, fp32 accumulation; a float result is summed from segments of 4096 elements of K in full float arithmetic (the
+ * tensor core truncates as it accumulates, about 1.1e-9 relative per element of K; a bf16 result is accumulated in one piece).
+ * A group may be empty and any length; variant 2 writes zeros for an empty one.  Rows of `out` outside every group (before offsets[0],
+ * from offsets[E] on) are left as they are.  Offsets are clamped to [0, T] and a falling one counts as the largest before it, so
+ * whatever they hold nothing outside the buffers is touched.  Rows of different groups never meet in a sum: infinities or NaN in
+ * one group's rows, or in rows of no group, stay out of the others' results.
+ * tail: out_dev, ldo, out_bf16 as in mbd_block_gemm_bf16; MBD_TAIL_STORE with bias_dev ([E][d_out] float, dense) and relu
+ * for variant 0; MBD_TAIL_MASK with mask_dev ([T, ldmask] in out's type) for variant 1; MBD_TAIL_SGD (out += scale * dW, Eq. 1)
+ * for variant 2; MBD_E_UNSUPPORTED for the others.  ReLU keeps a NaN.
+ * expert_stride: elements between the experts of W (variants 0, 1) or of dW (variant 2); not read for E = 1.
+ * d_in, d_out and T are free (T = 0: a tensor of no rows may be null); leading dimensions and expert_stride are multiples of 8, bases
+ * 16-byte aligned, E <= 512 (MBD_E_UNSUPPORTED otherwise, nothing is launched).  MBD_E_INVALID for leading dimensions or an
+ * expert_stride that would make rows or experts overlap.  status_dev as in mbd_block_gemm_bf16: NULL waits for the stream, a
+ * caller-owned zeroed word only enqueues (and may be captured into a graph).  The call keeps no state and no workspace. */
+MBD_API mbd_status mbd_expert_gemm_bf16(int variant, int E, const int32_t* offsets_dev, int64_t T, int64_t d_out, int64_t d_in,
+                                const void* A_dev, int64_t lda, const void* B_dev, int64_t ldb, int64_t expert_stride,
+                                const mbd_tail* tail, int32_t* status_dev, void* cuda_stream);
+
+/* ---- Products of 8-bit integers ----
+ * mbd_quantize_rows: for every row of X [R, K] (bf16 if x_bf16 != 0, else float), scale[r] = max |X_r| / 127 in float and
+ * Q[r, k] = X[r, k] / scale[r], correctly rounded to an integer (halves to even).  A row of zeros (or one whose scale underflows)
+ * has scale 0 and Q = 0; a row with an infinity or a NaN has scale NaN and Q = 0.  A row is a token of a batch or an output
+ * channel of a weight matrix; any alignment and any leading dimensions (16- and 8-byte accesses where they allow it).
+ * sync != 0: waits for the stream. */
+MBD_API mbd_status mbd_quantize_rows(const void* X_dev, int x_bf16, int64_t R, int64_t K, int64_t ldx, int8_t* Q_dev, int64_t ldq,
+                             float* scale_dev, int sync, void* cuda_stream);
+/* out[m, n] = act(a_scale[m] b_scale[n] sum_k A[m, k] B[n, k] (+ bias[n])): A [M, lda] int8 with a scale per row, B [N, ldb] int8 with a
+ * scale per output channel, exact int32 sums (K <= 131071, so that they cannot overflow; MBD_E_UNSUPPORTED beyond).  tail:
+ * MBD_TAIL_STORE with bias_dev and relu, out bf16 or float, ldo a multiple of 8.  lda, ldb multiples of 16, bases 16-byte aligned
+ * (MBD_E_UNSUPPORTED otherwise).  status_dev as above. */
+MBD_API mbd_status mbd_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t* A_dev, int64_t lda, const float* a_scale_dev,
+                       const int8_t* B_dev, int64_t ldb, const float* b_scale_dev, const mbd_tail* tail, int32_t* status_dev,
+                       void* cuda_stream);
+/* The same grouped by expert, variant 0 of mbd_expert_gemm_bf16: B [E][d_out, ldb], b_scale and bias [E][d_out], expert_stride a
+ * multiple of 16. */
+MBD_API mbd_status mbd_expert_gemm_i8(int E, const int32_t* offsets_dev, int64_t T, int64_t d_out, int64_t d_in, const int8_t* A_dev,
+                              int64_t lda, const float* a_scale_dev, const int8_t* B_dev, int64_t ldb, int64_t expert_stride,
+                              const float* b_scale_dev, const mbd_tail* tail, int32_t* status_dev, void* cuda_stream);
+
+/* ---- AdamW over many tensors ----
+ * One step over all tensors of a list in one launch, beside Eq. 1 and mbd_enable_momentum (Section 2: SGD stands for any first-order
+ * method).  With g = grad * grad_scale (gradients here are sums over the batch: grad_scale = 1 / B) and t = 1, 2, .. the step:
+ *     m <- b1 m + (1 - b1) g ,   v <- b2 v + (1 - b2) g^2
+ *     w <- w (1 - lr decay) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+ * in float; a bf16 weight is rounded once (from its float master if it has one, which is then what is updated).
+ * state_bits 32: m and v float [n].  state_bits 8: m and v are e4m3 numbers [n] (1 byte each), each block of 256 consecutive
+ * elements of a tensor has a float scale (m_scale, v_scale: [ceil(n / 256)]) that puts its largest finite value at 448; of v the
+ * ROOT is held (v = (code * scale)^2), never rounded from above zero to zero; an element that is not finite is held as NaN and
+ * leaves its block alone.  Zeroed buffers are the state before the first step, in both forms.
+ * The caller owns every buffer; the handle keeps the list and the step counter on the device current at creation, so a captured step
+ * counts on at each replay (lr and grad_scale are captured by value).  Tensors of any length and alignment (16-byte accesses where
+ * all of a tensor's bases allow it).  MBD_E_INVALID: an empty tensor, a missing pointer, a buffer that is written named twice or
+ * overlapping another, rates outside [0, 1), eps outside (0, 1), a negative decay, a master for float weights.  Steps of one handle
+ * must not overlap each other (one stream, or ordered streams).  MBD_E_STATE: the current device is not the handle's.
+ * set_steps / get_steps wait for the device. */
+typedef struct mbd_adamw mbd_adamw; /* opaque */
+typedef struct {
+  void* param_dev;           /* float, or bf16 if param_bf16 != 0                    */
+  float* master_dev;         /* float master of a bf16 weight, or NULL               */
+  const void* grad_dev;      /* float, or bf16 if grad_bf16 != 0                     */
+  void *m_dev, *v_dev;       /* float, or 1-byte codes                               */
+  float *m_scale_dev, *v_scale_dev; /* state_bits 8 only                             */
+  int64_t n;
+  float weight_decay;
+  int32_t param_bf16, grad_bf16, reserved;
+} mbd_adamw_tensor;
+MBD_API mbd_status mbd_adamw_create(const mbd_adamw_tensor* tensors_host, int count, int state_bits, double beta1, double beta2,
+                            double eps, int64_t steps_done, mbd_adamw** out);
+MBD_API mbd_status mbd_adamw_destroy(mbd_adamw* opt);
+MBD_API mbd_status mbd_adamw_step(mbd_adamw* opt, double lr, double grad_scale, void* cuda_stream);
+MBD_API mbd_status mbd_adamw_set_steps(mbd_adamw* opt, int64_t steps_done);
+MBD_API mbd_status mbd_adamw_get_steps(mbd_adamw* opt, int64_t* steps_done_host);
+
 /* ---- The convolution step piece by piece, for a driver with one process per row strip (Section 2.2) ----
  * A process holds its strip of every image as a network of its own (H = its rows) and exchanges the
  * strips' outer rows with its neighbours between the pieces: mbd_conv_stage_input, then per layer

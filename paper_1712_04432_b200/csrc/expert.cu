@@ -1,0 +1,903 @@
+// Products grouped by expert on the 5th-generation tensor cores (tcgen05): the three contractions of a layer
+// (Section 1 of the paper) where every row of the batch belongs to one of E experts with a weight matrix of its own,
+// and the product of 8-bit integers with a scale per row and per channel, dense or grouped.
+//
+//   variant 0  Y[r, :]  = X[r, :]  W_e^T          rows o[e] <= r < o[e+1]
+//   variant 1  dX[r, :] = dY[r, :] W_e
+//   variant 2  dW_e     = sum_{r in e} dY[r, :]^T X[r, :]
+//
+// The group sizes are known on the device only.  The output's CONTIGUOUS dimension (channels) takes the M side of the
+// instruction (128 rows per CTA, always full tiles of a weight matrix) and the output's rows the N side, which an
+// instruction takes in steps of 32: a ragged group of c rows costs ceil(c / 32) * 32 columns of tensor-core time, where
+// rows on the M side would cost ceil(c / 256) * 256.  The accumulator then has a channel per TMEM lane and an output
+// row per column, so that a warp stores 32 neighbouring channels of one row: full sectors without a staging tile, rows
+// behind a group's last one are just not stored, and bias and channel scale are one register per lane.
+//
+// One persistent CTA (or CTA pair, cta_group::2: 256 channels x up to 256 rows, each CTA loads its 128 channels and half
+// of the rows) per SM; warp roles as in the dense kernel: 0 TMA producer, 1 MMA issuer, 2..9 epilogue, and for
+// variant 2 a warp 10 that clears what the last k-block of a group holds of the next group (see `fixer`).
+// The split form cuts K over the CTAs of a cluster and joins the pieces through distributed shared memory, for calls
+// with too few tiles to keep the SMs busy.
+// Every wait is bounded; on time-out the kernel records a code and leaves.
+#include <stdlib.h>
+
+#include "../../include/mbd.h"
+#include "epi.cuh"
+#include "tc_common.cuh"
+
+namespace mbd {
+namespace {
+
+using namespace tc;
+
+constexpr int MAX_EXPERTS = 512;              // bounds and tile counts of all groups are held in shared memory
+constexpr int RING_BYTES = 192 * 1024;
+constexpr int CH = 128;                       // channels (M side) per CTA
+constexpr int A_BYTES = CH * 128;             // one k-block is 128 bytes of every row: 64 bf16 or 128 int8
+constexpr int SEG_BLOCKS = 64;                // k-blocks per accumulation segment of a float result, see Params::seg
+
+enum { KIND_BF16 = 0, KIND_I8 = 1 };
+
+struct Params {
+  int E, T;                  // experts; rows of the row tensors (offsets are clamped to [0, T])
+  const int32_t* offsets;    // [E + 1] on the device, or null: one group of all T rows
+  int M, N;                  // output channels; variant 2: output rows per expert (d_out)
+  int kb_total;              // variants 0, 1: k-blocks
+  int m_tiles, n_tiles;      // n_tiles: variant 2 only
+  int group_n;               // row tiles per raster group
+  int seg;                   // k-blocks per segment: the tensor core truncates when it adds to the accumulator (relative error
+                             // ~1.1e-9 per element of K, measured), so a float result is summed from segments of 4096 in
+                             // full float arithmetic; a bf16 result's rounding hides it
+  int op, out_bf16, relu;
+  void* out;
+  int64_t ldo, out_stride;   // out_stride: variant 2, elements between experts
+  const float* bias;         // [E][M] or null
+  const void* mask;
+  int64_t ldmask;
+  float scale;
+  const float* row_scale;    // i8: [T]
+  const float* ch_scale;     // i8: [E][M]
+  int* status;
+};
+
+// ------------------------------------------------------------------------------------------------ PTX forms
+__device__ __forceinline__ uint32_t cta_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t in_cta(uint32_t saddr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// Bounded wait for a barrier that another CTA of the pair arrives on after writing shared memory.
+__device__ __noinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+  const unsigned long long t0 = globaltimer_ns();
+  for (;;) {
+    for (int i = 0; i < 256; ++i) {
+      uint32_t ok;
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+      if (ok) return true;
+    }
+    if (*abort_flag) return false;
+    if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
+      *abort_flag = 1;
+      atomicCAS(status, 0, code);
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void load_3d_pair(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+template <int KIND, int PAIR>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+#define MBD_MMA(GROUP, TYPE)                                                                            \
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"                                        \
+               "tcgen05.mma.cta_group::" GROUP ".kind::" TYPE " [%0], %1, %2, %3, p;\n\t}"              \
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory")
+  if (KIND == KIND_BF16 && !PAIR) MBD_MMA("1", "f16");
+  if (KIND == KIND_BF16 && PAIR) MBD_MMA("2", "f16");
+  if (KIND == KIND_I8 && !PAIR) MBD_MMA("1", "i8");
+  if (KIND == KIND_I8 && PAIR) MBD_MMA("2", "i8");
+#undef MBD_MMA
+}
+template <int PAIR>
+__device__ __forceinline__ void commit(uint32_t bar) {
+  if (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"(static_cast<uint16_t>(3)) : "memory");
+  else
+    tc_commit(bar);
+}
+
+// ------------------------------------------------------------------------------------------------ work
+struct Unit {
+  int e, m0;                 // expert, first channel of the (pair's) tile
+  int row0, rows;            // first output row (variant 2: within dW_e) and how many exist
+  int nt;                    // columns of the instruction
+  int k0, kb, tail;          // variant 2: first row of the group, its k-blocks, rows in the last one
+};
+
+// Groups in shared memory: bound[e] .. bound[e+1] are the rows of expert e (the running maximum of the clamped offsets, so
+// that groups never overlap whatever the offsets hold), first[e] the row tiles of the experts before e.
+struct Groups {
+  int bound[MAX_EXPERTS + 1];
+  int first[MAX_EXPERTS + 1];
+};
+
+template <int BN>
+__device__ __forceinline__ void find_groups(const Params& p, Groups* g, int lane) {
+  int top = 0, tiles = 0;
+  for (int base = 0; base <= p.E; base += 32) {
+    const int i = base + lane;
+    int v = 0;
+    if (i <= p.E) v = p.offsets ? min(max(p.offsets[i], 0), p.T) : (i == 0 ? 0 : p.T);
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) v = max(v, o);
+    }
+    v = max(v, top);
+    int before = __shfl_up_sync(0xffffffffu, v, 1);
+    if (lane == 0) before = base == 0 ? v : top;
+    int t = i <= p.E ? (v - before + BN - 1) / BN : 0;          // tiles of expert i - 1
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, t, d);
+      if (lane >= d) t += o;
+    }
+    t += tiles;
+    if (i <= p.E) { g->bound[i] = v; g->first[i] = t; }
+    top = __shfl_sync(0xffffffffu, v, 31);
+    tiles = __shfl_sync(0xffffffffu, t, 31);
+  }
+}
+
+template <int B_MN, int BN, int PAIR>
+__device__ __forceinline__ int total_units(const Params& p, const Groups* g) {
+  return B_MN ? p.E * p.m_tiles * p.n_tiles : g->first[p.E] * p.m_tiles;
+}
+
+// Unit w of the launch; `e` is the expert of the unit before it (units come in rising order).
+template <int B_MN, int BN, int PAIR>
+__device__ __forceinline__ Unit unit_at(const Params& p, const Groups* g, int w, int& e) {
+  constexpr int STEP = B_MN ? (PAIR ? 128 : 64) : 32;
+  Unit u;
+  int local, tiles, count;
+  if (B_MN) {
+    tiles = p.n_tiles;
+    const int per = p.m_tiles * tiles;
+    e = w / per;
+    local = w - e * per;
+    count = p.N;
+  } else {
+    while (w >= g->first[e + 1] * p.m_tiles) ++e;
+    local = w - g->first[e] * p.m_tiles;
+    tiles = g->first[e + 1] - g->first[e];
+    count = g->bound[e + 1] - g->bound[e];
+  }
+  // raster groups of `group_n` row tiles, row tiles first: the operands of neighbouring units are shared in L2
+  const int per_group = p.group_n * p.m_tiles;
+  const int gi = local / per_group;
+  const int size = min(tiles - gi * p.group_n, p.group_n);
+  const int r = local - gi * per_group;
+  const int tn = gi * p.group_n + r % size;
+  // the rows of a group are dealt out evenly: the instruction's cost per column grows when columns are few
+  const int step = ((count + tiles - 1) / tiles + STEP - 1) / STEP * STEP;
+  u.e = e;
+  u.m0 = (r / size) * (PAIR ? 2 * CH : CH);
+  u.row0 = tn * step;
+  u.rows = min(step, count - u.row0);
+  u.nt = (u.rows + STEP - 1) / STEP * STEP;
+  u.k0 = 0;
+  u.kb = p.kb_total;
+  u.tail = 64;
+  if (B_MN) {
+    u.k0 = g->bound[e];
+    const int len = g->bound[e + 1] - u.k0;
+    u.kb = (len + 63) / 64;
+    u.tail = len - (u.kb - 1) * 64;
+  } else {
+    u.row0 += g->bound[e];
+  }
+  return u;
+}
+
+// ------------------------------------------------------------------------------------------------ epilogue
+__device__ __forceinline__ float relu(float x) { return x < 0.f ? 0.f : x; }        // (NaN stays NaN)
+
+// CNT output rows row0 .. of one channel per lane: r holds the accumulators of rows row0 + j.  `again`: the result so far
+// (the earlier segments of K) is in `out`; `last`: the tail operation is due.
+template <int KIND, int CNT>
+__device__ __forceinline__ void finish(const Params& p, const Unit& u, const uint32_t* r, int row0, int rows, int m, int lane,
+                                       float bias, float ch_scale, bool again, bool last) {
+  float v[CNT];
+  const int64_t base = u.row0 + row0;
+  if (KIND == KIND_I8) {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) {
+      const float s = j < rows ? p.row_scale[base + j] : 0.f;
+      v[j] = static_cast<float>(static_cast<int>(r[j])) * s * ch_scale;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) v[j] = __uint_as_float(r[j]);
+  }
+  if (p.out_bf16) {
+    // pairs of channels: the even lane of a pair takes row 2j, the odd lane row 2j + 1
+    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + u.e * p.out_stride;
+    const __nv_bfloat16* mask = reinterpret_cast<const __nv_bfloat16*>(p.mask);
+    const int odd = lane & 1, mp = m & ~1;
+    const bool two = mp + 1 < p.M, any = mp < p.M;
+    uint32_t x[CNT / 2];
+    const bool read = p.op == EPI_SGD || (p.op == EPI_MASK && mask != nullptr);
+    if (read) {
+      const __nv_bfloat16* src = p.op == EPI_SGD ? out : mask;
+      const int64_t ld = p.op == EPI_SGD ? p.ldo : p.ldmask;
+#pragma unroll
+      for (int j = 0; j < CNT / 2; ++j) {
+        const __nv_bfloat16* a = src + (base + 2 * j + odd) * ld + mp;
+        x[j] = 0;
+        if (2 * j + odd < rows) {
+          if (two) x[j] = *reinterpret_cast<const uint32_t*>(a);
+          else if (any) x[j] = *reinterpret_cast<const unsigned short*>(a);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < CNT / 2; ++j) {
+      float a = v[2 * j] + bias, b = v[2 * j + 1] + bias;
+      if (p.relu) { a = relu(a); b = relu(b); }
+      const float got = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
+      float lo = odd ? got : a, hi = odd ? b : got;
+      if (read) {
+        const float xl = bf16_bits_to_f32(x[j] & 0xFFFFu), xh = bf16_bits_to_f32(x[j] >> 16);
+        if (p.op == EPI_SGD) { lo = fmaf(p.scale, lo, xl); hi = fmaf(p.scale, hi, xh); }
+        else { if (!(xl > 0.f)) lo = 0.f; if (!(xh > 0.f)) hi = 0.f; }
+      }
+      if (2 * j + odd < rows) {
+        __nv_bfloat16* d = out + (base + 2 * j + odd) * p.ldo + mp;
+        if (two) *reinterpret_cast<uint32_t*>(d) = pack_bf16x2(lo, hi);
+        else if (any) *d = __float2bfloat16_rn(lo);
+      }
+    }
+    return;
+  }
+  float* out = reinterpret_cast<float*>(p.out) + u.e * p.out_stride + base * p.ldo + m;
+  const bool here = m < p.M;
+  const bool masked = p.op == EPI_MASK && p.mask != nullptr;
+  if (p.op == EPI_SGD || again || (masked && last)) {
+    float x[CNT], w[CNT];
+    const float* mask = reinterpret_cast<const float*>(p.mask) + base * p.ldmask + m;
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) {
+      x[j] = here && j < rows && (p.op == EPI_SGD || again) ? out[j * p.ldo] : 0.f;
+      w[j] = here && j < rows && masked && last ? mask[j * p.ldmask] : 1.f;
+    }
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) {
+      if (p.op == EPI_SGD) v[j] = fmaf(p.scale, v[j], x[j]);
+      else v[j] = w[j] > 0.f ? x[j] + v[j] : 0.f;
+    }
+  }
+  if (!here) return;
+#pragma unroll
+  for (int j = 0; j < CNT; ++j) {
+    if (last) {
+      v[j] += bias;
+      if (p.relu) v[j] = relu(v[j]);
+    }
+    if (j < rows) out[j * p.ldo] = v[j];
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ the kernel
+// KIND: bf16 or int8.  A (the M side) and B (the N side) are K-major (0) or MN-major (1, bf16 only).  B_MN is variant 2:
+// K is the rows of a group.  BN: most output rows of a tile.  PAIR: two CTAs share a tile of 256 channels.  SPLIT: one unit
+// per cluster, its K range cut over the CTAs.
+template <int KIND, int A_MN, int B_MN, int BN, int PAIR, int SPLIT>
+__global__ void __launch_bounds__(B_MN ? 352 : 320, 1)
+expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                   const __grid_constant__ CUtensorMap tmB32, const Params p) {
+  constexpr int BNL = PAIR ? BN / 2 : BN;
+  constexpr int STAGE_BYTES = A_BYTES + BNL * 128;
+  constexpr int STAGES = RING_BYTES / STAGE_BYTES;
+  constexpr int ACC_BUFS = SPLIT ? 1 : 2;
+  constexpr int TMEM_COLS = ACC_BUFS * BN;
+  constexpr int ELEMS = KIND == KIND_I8 ? 128 : 64;          // elements of a k-block
+  static_assert(TMEM_COLS >= 32 && TMEM_COLS <= 512 && STAGES <= 16, "");
+
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  __shared__ Groups groups;
+  __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES];
+  __shared__ __align__(8) uint64_t landed_bar[B_MN ? STAGES : 1], fixed_bar[B_MN ? STAGES : 1];
+  __shared__ __align__(8) uint64_t tmem_full_bar[2], tmem_empty_bar[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+
+  const uint32_t ring = smem_u32(smem_raw);
+  if (ring & 1023u) {                     // same answer in every CTA
+    if (threadIdx.x == 0) atomicCAS(p.status, 0, DEV_SMEM_MISALIGNED);
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = PAIR || SPLIT ? cta_rank() : 0u;
+  const int pieces = SPLIT ? static_cast<int>(cluster_size()) : 1;
+  const int w_first = PAIR ? blockIdx.x >> 1 : SPLIT ? blockIdx.x / pieces : blockIdx.x;
+  const int w_step = PAIR ? gridDim.x >> 1 : SPLIT ? 1 << 30 : gridDim.x;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(smem_u32(&full_bar[i]), 1);
+      mbar_init(smem_u32(&empty_bar[i]), 1);
+      if (B_MN) {
+        mbar_init(smem_u32(&landed_bar[i]), 1);
+        mbar_init(smem_u32(&fixed_bar[i]), PAIR ? 2 : 1);
+      }
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&tmem_full_bar[i]), 1);
+      mbar_init(smem_u32(&tmem_empty_bar[i]), PAIR ? 16 : 8);
+    }
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(TMEM_COLS) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      tmem_alloc<TMEM_COLS>(smem_u32(&tmem_slot));
+    }
+  }
+  pdl_trigger();
+  pdl_wait();                              // the offsets may come from the kernel before this one
+  if (warp == 0) find_groups<BN>(p, &groups, lane);
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR || SPLIT) cluster_sync();       // the other CTAs' barriers exist before anything remote touches them
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+  const int total = total_units<B_MN, BN, PAIR>(p, &groups);
+  volatile int* abortp = &abort_flag;
+  int expert = 0;
+
+  // k-blocks of this CTA's share of a unit
+  auto first_kb = [&](const Unit& u) { return SPLIT ? static_cast<int>(static_cast<long long>(rank) * u.kb / pieces) : 0; };
+  auto last_kb = [&](const Unit& u) { return SPLIT ? static_cast<int>(static_cast<long long>(rank + 1) * u.kb / pieces) : u.kb; };
+  // the last k-block of a group of rows holds rows of the next group, and an instruction takes 16
+  auto ragged = [&](const Unit& u, int kb) { return B_MN && kb == u.kb - 1 && (u.tail & 15) != 0; };
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int w = w_first; w < total && ok; w += w_step) {
+        const Unit u = unit_at<B_MN, BN, PAIR>(p, &groups, w, expert);
+        const int m = u.m0 + (PAIR ? static_cast<int>(rank) * CH : 0);
+        const int half = PAIR ? u.nt / 2 : u.nt;                      // output rows this CTA loads
+        const int n = u.row0 + (PAIR ? static_cast<int>(rank) * half : 0);
+        const bool whole = half > BNL / 2;                            // one box of BNL rows, or boxes of 32
+        const int boxes = B_MN ? half / 64 : whole ? 1 : (half + 31) / 32;
+        const uint32_t bytes = A_BYTES + (B_MN ? boxes * 8192u : whole ? BNL * 128u : boxes * 4096u);
+        const int kb1 = last_kb(u);
+        for (int kb = first_kb(u); kb < kb1; ++kb) {
+          ok = mbar_wait(smem_u32(&empty_bar[stage]), phase ^ 1u, abortp, p.status, DEV_TIMEOUT_PRODUCER);
+          if (!ok) break;
+          const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + A_BYTES;
+          const bool rag = ragged(u, kb);
+          const bool pair_bar = PAIR && !rag;
+          uint32_t bar = smem_u32(&full_bar[stage]);
+          if (rag) {                       // each CTA of a pair learns of its own bytes; the stage is full when both have cleared it
+            if (rank == 0 || !PAIR) mbar_arrive(bar);
+            bar = smem_u32(&landed_bar[stage]);
+            mbar_expect_tx(bar, bytes);
+          } else if (!PAIR) {
+            mbar_expect_tx(bar, bytes);
+          } else {
+            if (rank == 0) mbar_expect_tx(bar, 2 * bytes);
+            bar = in_cta(bar, 0);
+          }
+          auto load = [&](uint32_t dst, const CUtensorMap* tm, int x, int y, int z) {
+            if (pair_bar) load_3d_pair(dst, tm, x, y, z, bar);
+            else load_3d(dst, tm, x, y, z, bar);
+          };
+          const int k = B_MN ? u.k0 + kb * 64 : kb * ELEMS;
+          const int ez = B_MN ? 0 : u.e;
+          if (A_MN == 0) {
+            load(sa, &tmA, k, m, ez);
+          } else {
+#pragma unroll
+            for (int c = 0; c < CH / 64; ++c) load(sa + c * 8192, &tmA, m + c * 64, k, ez);
+          }
+          if (B_MN) {
+            for (int c = 0; c < boxes; ++c) load(sb + c * 8192, &tmB, n + c * 64, k, 0);
+          } else if (whole) {
+            load(sb, &tmB, k, n, 0);
+          } else {
+            for (int c = 0; c < boxes; ++c) load(sb + c * 4096, &tmB32, k, n + c * 32, 0);
+          }
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer
+    if (lane == 0 && (!PAIR || rank == 0)) {
+      int stage = 0, it = 0;
+      uint32_t phase = 0, fixed_phase = 0;                 // fixed_phase: one bit per stage
+      bool ok = true;
+      for (int w = w_first; w < total && ok; w += w_step) {
+        const Unit u = unit_at<B_MN, BN, PAIR>(p, &groups, w, expert);
+        const uint32_t idesc = (KIND == KIND_I8 ? (2u << 4) | (1u << 7) | (1u << 10)
+                                                : (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(A_MN) << 15) | (uint32_t(B_MN) << 16)) |
+                               (static_cast<uint32_t>(u.nt >> 3) << 17) | (uint32_t((PAIR ? 2 * CH : CH) >> 4) << 24);
+        const int kb1 = last_kb(u);
+        int kb = first_kb(u);
+        while (kb < kb1 && ok) {                           // a segment
+          const int seg_end = min(kb1, kb + p.seg);
+          const int acc = it % ACC_BUFS;
+          ok = mbar_wait(smem_u32(&tmem_empty_bar[acc]), ((it / ACC_BUFS) & 1u) ^ 1u, abortp, p.status, DEV_TIMEOUT_MMA_TMEM);
+          if (!ok) break;
+          ++it;
+          tc_fence_after();
+          const uint32_t d = tmem_base + acc * BN;
+          bool add = false;
+          for (; kb < seg_end; ++kb) {
+            ok = mbar_wait(smem_u32(&full_bar[stage]), phase, abortp, p.status, DEV_TIMEOUT_MMA_FULL);
+            if (!ok) break;
+            if (ragged(u, kb)) {
+              ok = wait_cluster(smem_u32(&fixed_bar[stage]), (fixed_phase >> stage) & 1u, abortp, p.status, DEV_TIMEOUT_MMA_FULL);
+              if (!ok) break;
+              fixed_phase ^= 1u << stage;
+            }
+            tc_fence_after();
+            const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + A_BYTES;
+            const uint64_t ad = A_MN ? make_desc(sa, 8192, 1024) : make_desc(sa, 16, 1024);
+            const uint64_t bd = B_MN ? make_desc(sb, 8192, 1024) : make_desc(sb, 16, 1024);
+            constexpr uint64_t A_STEP = (A_MN ? 2048 : 32) >> 4, B_STEP = (B_MN ? 2048 : 32) >> 4;
+            const int steps = B_MN && kb == u.kb - 1 ? (u.tail + 15) >> 4 : 4;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (!B_MN || k < steps) {
+                mma<KIND, PAIR>(d, ad + k * A_STEP, bd + k * B_STEP, idesc, add ? 1u : 0u);
+                add = true;
+              }
+            }
+            commit<PAIR>(smem_u32(&empty_bar[stage]));
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          }
+          if (ok) commit<PAIR>(smem_u32(&tmem_full_bar[acc]));
+        }
+      }
+    }
+  } else if (warp < 10) {
+    // ------------------------------------------------------------------ epilogue
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    if (SPLIT) {
+      if (w_first < total) {
+        const Unit u = unit_at<B_MN, BN, PAIR>(p, &groups, w_first, expert);
+        if (first_kb(u) < last_kb(u)) (void)mbar_wait(smem_u32(&tmem_full_bar[0]), 0, abortp, p.status, DEV_TIMEOUT_EPILOGUE);
+        __syncwarp();
+      }
+    } else {
+      int it = 0;
+      bool ok = true;
+      for (int w = w_first; w < total && ok; w += w_step) {
+        const Unit u = unit_at<B_MN, BN, PAIR>(p, &groups, w, expert);
+        const int m = u.m0 + (PAIR ? static_cast<int>(rank) * CH : 0) + q * 32 + lane;
+        const float bias = p.bias && m < p.M ? p.bias[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
+        const float cs = KIND == KIND_I8 && m < p.M ? p.ch_scale[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
+        if (u.kb == 0) {                                   // an expert without rows: its gradient is zero
+          uint32_t r[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) r[j] = 0;
+          for (int c = half; c * 32 < u.rows; c += 2) finish<KIND, 32>(p, u, r, c * 32, u.rows - c * 32, m, lane, bias, cs, false, true);
+          continue;
+        }
+        for (int kb = 0; kb < u.kb && ok; kb += p.seg, ++it) {
+          const bool last = kb + p.seg >= u.kb;
+          const int acc = it % ACC_BUFS;
+          ok = mbar_wait(smem_u32(&tmem_full_bar[acc]), (it / ACC_BUFS) & 1u, abortp, p.status, DEV_TIMEOUT_EPILOGUE);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * BN;
+          const int chunks = (u.rows + 31) / 32;
+          for (int c = half; c < chunks; c += 2) {
+            uint32_t r[32];
+            tc_ld32(taddr + c * 32, r);
+            tc_wait_ld();
+            if (c + 2 >= chunks) {                         // all of the accumulator read: hand it back
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) arrive_cluster(in_cta(smem_u32(&tmem_empty_bar[acc]), 0));
+            }
+            finish<KIND, 32>(p, u, r, c * 32, u.rows - c * 32, m, lane, bias, cs, kb > 0, last);
+          }
+          if (half >= chunks) {                            // nothing to read for this warp
+            __syncwarp();
+            if (lane == 0) arrive_cluster(in_cta(smem_u32(&tmem_empty_bar[acc]), 0));
+          }
+        }
+      }
+    }
+  } else if (B_MN) {
+    // ------------------------------------------------------------------ fixer
+    // A group's last k-block ends with rows of the next group (or behind the last group).  They are no zeros, and may be
+    // infinities or NaN, so multiplying them by zeros would not do: both operands' rows up to the next multiple of 16 are
+    // cleared in shared memory before the instruction reads them.  A row of a swizzled chunk is 128 bytes whatever the swizzle.
+    int stage = 0;
+    uint32_t landed_phase = 0;
+    bool ok = true;
+    for (int w = w_first; w < total && ok; w += w_step) {
+      const Unit u = unit_at<B_MN, BN, PAIR>(p, &groups, w, expert);
+      const int kb0 = first_kb(u), kb1 = last_kb(u);
+      if (kb1 > kb0) {
+        const int s = (stage + kb1 - 1 - kb0) % STAGES;
+        if (ragged(u, kb1 - 1)) {
+          ok = mbar_wait(smem_u32(&landed_bar[s]), (landed_phase >> s) & 1u, abortp, p.status, DEV_TIMEOUT_PRODUCER);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          landed_phase ^= 1u << s;
+          const int rows = ((u.tail + 15) & ~15) - u.tail;
+          const int chunks = CH / 64 + (PAIR ? u.nt / 2 : u.nt) / 64;
+          uint8_t* base = smem_raw + s * STAGE_BYTES;
+          for (int i = lane; i < chunks * rows * 8; i += 32) {
+            const int c = i / (rows * 8), v = i - c * (rows * 8);
+            *reinterpret_cast<uint4*>(base + c * 8192 + u.tail * 128 + v * 16) = make_uint4(0, 0, 0, 0);
+          }
+          asm volatile("fence.proxy.async;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) arrive_cluster(in_cta(smem_u32(&fixed_bar[s]), PAIR ? 0 : rank));
+        }
+        stage = (stage + kb1 - kb0) % STAGES;
+      }
+    }
+  }
+
+  if (SPLIT) {
+    // The pieces of K meet in the cluster's shared memory: the CTA with rank g % pieces adds the pieces of output rows
+    // 8 g .. 8 g + 7 in ascending order and finishes them.  The ring is idle in every CTA once its accumulator is complete.
+    __syncwarp();
+    cluster_sync();
+    const bool work = w_first < total;
+    Unit u{};
+    if (work && warp >= 2 && warp < 10) {
+      expert = 0;
+      u = unit_at<B_MN, BN, PAIR>(p, &groups, w_first, expert);
+    }
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    const int eights = work ? (u.rows + 7) / 8 : 0;
+    const int own_max = (BN / 8 + pieces - 1) / pieces;
+    if (work && warp >= 2 && warp < 10) {
+      const bool some = first_kb(u) < last_kb(u);
+      tc_fence_after();
+      for (int g = half; g < eights; g += 2) {
+        uint32_t r[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (some) {
+          tc_ld8(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + g * 8, r);
+          tc_wait_ld();
+        }
+        const uint32_t at = in_cta(ring + (((rank * own_max + g / pieces) * 8) * CH + q * 32 + lane) * 4, g % pieces);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at + j * CH * 4), "r"(r[j]) : "memory");
+      }
+    }
+    __syncwarp();
+    cluster_sync();
+    if (work && warp >= 2 && warp < 10) {
+      const int m = u.m0 + q * 32 + lane;
+      const float bias = p.bias && m < p.M ? p.bias[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
+      const float cs = KIND == KIND_I8 && m < p.M ? p.ch_scale[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
+      for (int o = half; o * pieces + static_cast<int>(rank) < eights; o += 2) {
+        const int g = o * pieces + rank;
+        uint32_t r[8];
+        for (int s = 0; s < pieces; ++s) {
+          const uint32_t* src = reinterpret_cast<const uint32_t*>(smem_raw) + ((s * own_max + o) * 8) * CH + q * 32 + lane;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t x = src[j * CH];
+            if (s == 0) r[j] = x;
+            else if (KIND == KIND_I8) r[j] += x;
+            else r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(x));
+          }
+        }
+        finish<KIND, 8>(p, u, r, g * 8, u.rows - g * 8, m, lane, bias, cs, false, true);
+      }
+    }
+  }
+
+  if (abort_flag && threadIdx.x == 0) {    // a wait ran out: let the copies in flight land before shared memory is given back
+    const unsigned long long t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 1000000ull) {}
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync();                // the other CTA may still signal barriers in this one's shared memory
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+    else tmem_dealloc<TMEM_COLS>(tmem_base);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static const EncodeTiledFn fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) f = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(f);
+  }();
+  return fn;
+}
+
+// [depth][rows][inner] with row stride `ld` and plane stride `plane` in elements of `esize` bytes; 128 bytes per box row.
+bool make_map(CUtensorMap* tm, const void* base, int esize, uint64_t inner, uint64_t rows, uint64_t depth, uint64_t ld, uint64_t plane,
+              uint32_t box_rows) {
+  const cuuint64_t dims[3] = {inner, rows, depth};
+  const cuuint64_t strides[2] = {ld * esize, plane * esize};
+  const cuuint32_t box[3] = {128u / esize, box_rows, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return encode_fn()(tm, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
+                     strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int MAX_DEVICES = 64;
+
+struct Launch {
+  int BN, pair, split;       // split: CTAs that share a unit's K range; 0: the persistent form
+  int grid;
+};
+
+template <int KIND, int A_MN, int B_MN>
+cudaError_t set_attributes() {
+  cudaError_t e;
+  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES)) != cudaSuccess) return e;
+  return cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES);
+}
+
+cudaError_t init(int dev) {
+  static bool done[MAX_DEVICES] = {false};       // the opt-in to large shared memory is per device; setting it twice does no harm
+  if (dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
+  if (done[dev]) return cudaSuccess;
+  if (!encode_fn()) return cudaErrorNotSupported;
+  cudaError_t e;
+  if ((e = set_attributes<KIND_BF16, 0, 0>()) != cudaSuccess) return e;
+  if ((e = set_attributes<KIND_BF16, 1, 0>()) != cudaSuccess) return e;
+  if ((e = set_attributes<KIND_BF16, 1, 1>()) != cudaSuccess) return e;
+  if ((e = set_attributes<KIND_I8, 0, 0>()) != cudaSuccess) return e;
+  done[dev] = true;
+  return cudaSuccess;
+}
+
+template <int KIND, int A_MN, int B_MN>
+cudaError_t launch(const Launch& l, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b32, const Params& p, cudaStream_t stream) {
+  const dim3 grid(l.grid), block(B_MN ? 352 : 320);
+  if (l.pair) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, grid, block, RING_BYTES, stream, 2, a, b, b32, p);
+  if (!l.split) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, grid, block, RING_BYTES, stream, 1, a, b, b32, p);
+  return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, grid, block, RING_BYTES, stream, l.split, a, b, b32, p);
+}
+
+// Most units a call can have: a group of c rows is cut into ceil(c / BN) row tiles.
+int64_t most_units(int variant, int E, int64_t T, int64_t M, int64_t N, int BN, int ch) {
+  const int64_t mt = (M + ch - 1) / ch;
+  if (variant == 2) return E * mt * ((N + BN - 1) / BN);
+  const int64_t groups = E < T ? E : T;
+  return mt * (E == 1 ? (T + BN - 1) / BN : T / BN + groups);
+}
+
+Launch plan(int kind, int variant, int E, int64_t T, int64_t M, int64_t N, int64_t K, bool out_f32, int sms) {
+  Launch l{256, 1, 0, 0};
+  const int64_t rows = variant == 2 ? N : (T + E - 1) / E;       // output rows of a group, on average
+  const int64_t per_kb = kind == KIND_I8 ? 128 : 64;
+  const int64_t k = variant == 2 ? (T + E - 1) / E : K;
+  if (rows <= 64) {
+    l.BN = 64;
+    l.pair = 0;
+    const int64_t units = most_units(variant, E, T, M, N, 64, CH);
+    const int64_t kbs = (k + per_kb - 1) / per_kb;
+    int s = 0;
+    for (int c = 2; c <= 8; c *= 2)
+      if (units * c <= sms && kbs / c >= 4) s = c;
+    if (out_f32 && kind == KIND_BF16 && s && (variant == 2 ? T : K) / s > 64 * SEG_BLOCKS) s = 0;
+    l.split = s;
+  }
+  const int64_t units = most_units(variant, E, T, M, N, l.BN, l.pair ? 2 * CH : CH);
+  if (l.split) l.grid = static_cast<int>(units * l.split);
+  else if (l.pair) l.grid = static_cast<int>(2 * (units < sms / 2 ? units : sms / 2));
+  else l.grid = static_cast<int>(units < sms ? units : sms);
+  return l;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+struct Call {
+  int kind, variant, E;
+  const int32_t* offsets;
+  int64_t T, d_out, d_in;
+  const void* A; int64_t lda;           // rows: X or dY
+  const void* B; int64_t ldb;           // W, or (variant 2) X
+  int64_t stride;                       // elements between experts of W, or of dW
+  const float* row_scale; const float* ch_scale;
+  const mbd_tail* tail;
+  int32_t* status;
+  void* stream;
+};
+
+mbd_status run(Call c) {
+  const mbd_tail* t = c.tail;
+  mbd_tail tail;
+  if (t && c.T == 0) {                                          // no rows: the row tensors may be null, and are not read
+    tail = *t;
+    t = &tail;
+    if (c.variant != 2 && !tail.out_dev) tail.out_dev = const_cast<void*>(c.B);
+    if (!c.A) c.A = t->out_dev;
+    if (!c.B && c.variant == 2) c.B = t->out_dev;
+  }
+  if (!c.A || !c.B || !t || !t->out_dev || c.variant < 0 || c.variant > 2 || c.E < 1 || c.T < 0 || c.d_out < 1 || c.d_in < 1) return MBD_E_INVALID;
+  if (t->op != MBD_TAIL_STORE && t->op != MBD_TAIL_MASK && t->op != MBD_TAIL_SGD) return MBD_E_INVALID;
+  if (!c.offsets && c.E != 1) return MBD_E_INVALID;
+  if (c.kind == KIND_I8 && (!c.row_scale || !c.ch_scale)) return MBD_E_INVALID;
+  const int unit = c.kind == KIND_I8 ? 16 : 8;                  // elements of 16 bytes
+  const int64_t cols_a = c.variant == 0 ? c.d_in : c.d_out, cols_b = c.d_in;
+  const int64_t M = c.variant == 0 ? c.d_out : c.d_in;          // channels of the result
+  const int64_t N = c.variant == 2 ? c.d_out : 0;
+  if (c.lda < cols_a || c.ldb < cols_b || t->ldo < M || (t->mask_dev && t->ldmask < M)) return MBD_E_INVALID;
+  const int64_t plane_rows = c.d_out;
+  if (c.E > 1 && c.stride < (plane_rows - 1) * (c.variant == 2 ? t->ldo : c.ldb) + c.d_in) return MBD_E_INVALID;   // experts would overlap
+  if (c.E > MAX_EXPERTS || c.T > INT32_MAX - 1024 || c.d_out > INT32_MAX - 1024 || c.d_in > INT32_MAX - 1024) return MBD_E_UNSUPPORTED;
+  if (c.kind == KIND_I8 && c.d_in > 131071) return MBD_E_UNSUPPORTED;        // 128 * 128 * d_in stays below 2^31
+  if (c.lda % unit || c.ldb % unit || t->ldo % 8 || (t->mask_dev && t->ldmask % 8) || (c.E > 1 && c.stride % unit)) return MBD_E_UNSUPPORTED;
+  if (!aligned16(c.A) || !aligned16(c.B) || !aligned16(t->out_dev) || !aligned16(t->mask_dev)) return MBD_E_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(t->bias_dev) | reinterpret_cast<uintptr_t>(c.offsets) | reinterpret_cast<uintptr_t>(c.row_scale) |
+       reinterpret_cast<uintptr_t>(c.ch_scale)) & 3u) return MBD_E_UNSUPPORTED;
+  // each tail operation belongs to one product: bias and ReLU to the forward one, the mask to backward-data, Eq. 1 to
+  // backward-weight
+  if ((t->bias_dev || t->relu) && c.variant != 0) return MBD_E_UNSUPPORTED;
+  if (t->op == MBD_TAIL_MASK && c.variant != 1) return MBD_E_UNSUPPORTED;
+  if (t->op == MBD_TAIL_SGD && c.variant != 2) return MBD_E_UNSUPPORTED;
+  const int64_t groups = c.E < c.T ? c.E : c.T;
+  const int64_t mt = (M + CH - 1) / CH;
+  if (c.variant == 2 ? static_cast<double>(c.E) * mt * ((N + 63) / 64) > 1e9 : static_cast<double>(mt) * (c.T / 64 + groups + 1) > 1e9) return MBD_E_UNSUPPORTED;
+  if (c.T == 0 && c.variant != 2) return MBD_OK;                // no rows, nothing to write
+
+  int dev = 0, sms = 0, major = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return MBD_E_CUDA;
+  }
+  if (major != 10) return MBD_E_UNSUPPORTED;
+  if (init(dev) != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_CUDA; }
+  cudaStream_t stream = static_cast<cudaStream_t>(c.stream);
+
+  Launch l = plan(c.kind, c.variant, c.E, c.T, M, N, c.d_in, !t->out_bf16, sms);
+  if (c.variant == 1) l = plan(c.kind, 1, c.E, c.T, M, N, c.d_out, !t->out_bf16, sms);
+  const int bnl = l.pair ? l.BN / 2 : l.BN;
+  const int esize = c.kind == KIND_I8 ? 1 : 2;
+  const uint64_t plane = c.E > 1 ? static_cast<uint64_t>(c.stride) : static_cast<uint64_t>(c.d_out) * c.ldb;
+  const uint64_t rows = c.T > 0 ? c.T : 1;                      // (a map of no rows cannot be described; nothing is loaded then)
+  CUtensorMap a, b, b32;
+  bool ok;
+  if (c.variant == 0) {
+    ok = make_map(&a, c.B, esize, c.d_in, c.d_out, c.E, c.ldb, plane, CH) &&
+         make_map(&b, c.A, esize, c.d_in, rows, 1, c.lda, rows * c.lda, bnl) && make_map(&b32, c.A, esize, c.d_in, rows, 1, c.lda, rows * c.lda, 32);
+  } else if (c.variant == 1) {
+    ok = make_map(&a, c.B, esize, c.d_in, c.d_out, c.E, c.ldb, plane, 64) &&
+         make_map(&b, c.A, esize, c.d_out, rows, 1, c.lda, rows * c.lda, bnl) && make_map(&b32, c.A, esize, c.d_out, rows, 1, c.lda, rows * c.lda, 32);
+  } else {
+    ok = make_map(&a, c.B, esize, c.d_in, rows, 1, c.ldb, rows * c.ldb, 64) && make_map(&b, c.A, esize, c.d_out, rows, 1, c.lda, rows * c.lda, 64);
+    b32 = b;
+  }
+  if (!ok) return MBD_E_CUDA;
+
+  Params p{};
+  p.E = c.E; p.T = static_cast<int>(c.T);
+  p.offsets = c.offsets;
+  p.M = static_cast<int>(M); p.N = static_cast<int>(N);
+  const int64_t K = c.variant == 0 ? c.d_in : c.d_out;
+  const int per_kb = c.kind == KIND_I8 ? 128 : 64;
+  p.kb_total = static_cast<int>((K + per_kb - 1) / per_kb);
+  p.m_tiles = static_cast<int>((M + (l.pair ? 2 * CH : CH) - 1) / (l.pair ? 2 * CH : CH));
+  p.n_tiles = static_cast<int>((N + l.BN - 1) / l.BN);
+  p.group_n = 8;
+  p.seg = c.kind == KIND_BF16 && !t->out_bf16 && !l.split ? SEG_BLOCKS : 1 << 30;
+  p.op = t->op == MBD_TAIL_STORE ? EPI_ACT : t->op == MBD_TAIL_MASK ? EPI_MASK : EPI_SGD;
+  p.out_bf16 = t->out_bf16 != 0;
+  p.relu = t->relu != 0;
+  p.out = t->out_dev;
+  p.ldo = t->ldo;
+  p.out_stride = c.variant == 2 ? (c.E > 1 ? c.stride : 0) : 0;
+  p.bias = t->bias_dev;
+  p.mask = t->op == MBD_TAIL_MASK ? t->mask_dev : nullptr;
+  p.ldmask = t->ldmask;
+  p.scale = t->scale;
+  p.row_scale = c.row_scale;
+  p.ch_scale = c.ch_scale;
+
+  int* word = c.status;
+  if (!word) {
+    if (cudaMalloc(reinterpret_cast<void**>(&word), sizeof(int)) != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_ALLOC; }
+    if (cudaMemsetAsync(word, 0, sizeof(int), stream) != cudaSuccess) { (void)cudaGetLastError(); cudaFree(word); return MBD_E_CUDA; }
+  }
+  p.status = word;
+  cudaError_t e;
+  if (c.kind == KIND_I8) e = launch<KIND_I8, 0, 0>(l, a, b, b32, p, stream);
+  else if (c.variant == 0) e = launch<KIND_BF16, 0, 0>(l, a, b, b32, p, stream);
+  else if (c.variant == 1) e = launch<KIND_BF16, 1, 0>(l, a, b, b32, p, stream);
+  else e = launch<KIND_BF16, 1, 1>(l, a, b, b32, p, stream);
+  mbd_status ret = e == cudaSuccess ? MBD_OK : MBD_E_CUDA;
+  if (c.status) {                          // enqueue-only: the caller owns and reads the status word
+    if (ret != MBD_OK) (void)cudaGetLastError();
+    return ret;
+  }
+  int h = 0;
+  if (ret == MBD_OK) {
+    if (cudaStreamSynchronize(stream) != cudaSuccess || cudaMemcpy(&h, word, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) ret = MBD_E_CUDA;
+    else if (h != 0) ret = h == DEV_SMEM_MISALIGNED ? MBD_E_CUDA : MBD_E_TIMEOUT;
+  }
+  (void)cudaGetLastError();
+  cudaFree(word);
+  return ret;
+}
+
+}  // namespace
+}  // namespace mbd
+
+using namespace mbd;
+
+extern "C" mbd_status mbd_expert_gemm_bf16(int variant, int E, const int32_t* offsets_dev, int64_t T, int64_t d_out, int64_t d_in,
+                                           const void* A_dev, int64_t lda, const void* B_dev, int64_t ldb, int64_t expert_stride,
+                                           const mbd_tail* tail, int32_t* status_dev, void* cuda_stream) {
+  if (!offsets_dev) return MBD_E_INVALID;
+  return run(Call{KIND_BF16, variant, E, offsets_dev, T, d_out, d_in, A_dev, lda, B_dev, ldb, expert_stride, nullptr, nullptr, tail,
+                  status_dev, cuda_stream});
+}
+
+extern "C" mbd_status mbd_expert_gemm_i8(int E, const int32_t* offsets_dev, int64_t T, int64_t d_out, int64_t d_in, const int8_t* A_dev,
+                                         int64_t lda, const float* a_scale_dev, const int8_t* B_dev, int64_t ldb, int64_t expert_stride,
+                                         const float* b_scale_dev, const mbd_tail* tail, int32_t* status_dev, void* cuda_stream) {
+  if (!offsets_dev) return MBD_E_INVALID;
+  return run(Call{KIND_I8, 0, E, offsets_dev, T, d_out, d_in, A_dev, lda, B_dev, ldb, expert_stride, a_scale_dev, b_scale_dev, tail,
+                  status_dev, cuda_stream});
+}
+
+extern "C" mbd_status mbd_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t* A_dev, int64_t lda, const float* a_scale_dev,
+                                  const int8_t* B_dev, int64_t ldb, const float* b_scale_dev, const mbd_tail* tail, int32_t* status_dev,
+                                  void* cuda_stream) {
+  if (M < 1) return MBD_E_INVALID;
+  return run(Call{KIND_I8, 0, 1, nullptr, M, N, K, A_dev, lda, B_dev, ldb, 0, a_scale_dev, b_scale_dev, tail, status_dev, cuda_stream});
+}

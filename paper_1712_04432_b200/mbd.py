@@ -31,7 +31,9 @@ EXPORTS = ["mbd_net_create", "mbd_net_destroy", "mbd_set_weights", "mbd_get_weig
            "mbd_comm_time", "mbd_redistribute_time", "mbd_total_time", "mbd_grid_table", "mbd_choose_grid",
            "mbd_enable_master_weights", "mbd_enable_momentum", "mbd_block_gemm_bf16", "mbd_block_reduce", "mbd_softmax_xent",
            "mbd_conv_stage_input", "mbd_conv_forward_layer", "mbd_conv_backward_layer", "mbd_conv_outer_rows",
-           "mbd_get_plan", "mbd_plan_product", "mbd_conv_forward_layer_rows", "mbd_conv_backward_layer_rows"]
+           "mbd_get_plan", "mbd_plan_product", "mbd_conv_forward_layer_rows", "mbd_conv_backward_layer_rows",
+           "mbd_expert_gemm_bf16", "mbd_quantize_rows", "mbd_gemm_i8", "mbd_expert_gemm_i8",
+           "mbd_adamw_create", "mbd_adamw_destroy", "mbd_adamw_step", "mbd_adamw_set_steps", "mbd_adamw_get_steps"]
 
 
 class MbdError(RuntimeError):
@@ -81,6 +83,13 @@ class Times(C.Structure):
 class GridRow(C.Structure):
     _fields_ = [("P_r", C.c_int32), ("P_c", C.c_int32), ("comm_fwd", C.c_double), ("comm_bwd", C.c_double),
                 ("comm", C.c_double), ("total", C.c_double)]
+
+
+class AdamWTensor(C.Structure):
+    """mbd_adamw_tensor: one entry of an AdamW list (see include/mbd.h)."""
+    _fields_ = [("param_dev", C.c_void_p), ("master_dev", C.c_void_p), ("grad_dev", C.c_void_p), ("m_dev", C.c_void_p),
+                ("v_dev", C.c_void_p), ("m_scale_dev", C.c_void_p), ("v_scale_dev", C.c_void_p), ("n", C.c_int64),
+                ("weight_decay", C.c_float), ("param_bf16", C.c_int32), ("grad_bf16", C.c_int32), ("reserved", C.c_int32)]
 
 
 GRID_UNIFORM, GRID_CONV_BATCH = 0, 1
@@ -144,6 +153,15 @@ def lib():
         L.mbd_plan_product.argtypes = [i32, i64, i64, i64, i32, i32, i32, C.POINTER(Plan)]
         L.mbd_gemm_bf16.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp]
         L.mbd_gemm_bf16_noalloc.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, i32, vp]
+        L.mbd_expert_gemm_bf16.argtypes = [i32, i32, vp, i64, i64, i64, vp, i64, vp, i64, i64, C.POINTER(Tail), vp, vp]
+        L.mbd_quantize_rows.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i32, vp]
+        L.mbd_gemm_i8.argtypes = [i64, i64, i64, vp, i64, vp, vp, i64, vp, C.POINTER(Tail), vp, vp]
+        L.mbd_expert_gemm_i8.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, vp, i64, i64, vp, C.POINTER(Tail), vp, vp]
+        L.mbd_adamw_create.argtypes = [C.POINTER(AdamWTensor), i32, i32, f64, f64, f64, i64, C.POINTER(vp)]
+        L.mbd_adamw_destroy.argtypes = [vp]
+        L.mbd_adamw_step.argtypes = [vp, f64, f64, vp]
+        L.mbd_adamw_set_steps.argtypes = [vp, i64]
+        L.mbd_adamw_get_steps.argtypes = [vp, C.POINTER(i64)]
         L.mbd_selftest_timeout.argtypes = [i32, vp]
         L.mbd_strerror.argtypes = [i32]
         L.mbd_strerror.restype = C.c_char_p
@@ -528,6 +546,178 @@ def softmax_xent(logits, labels, dY, per_sample, sync: bool = True):
     Bn, d = logits.shape
     _check(lib().mbd_softmax_xent(_ptr(logits), Bn, d, _ptr(labels), _ptr(dY), int(dY.dtype == torch.bfloat16),
                                   _ptr(per_sample), int(sync), _stream()), "mbd_softmax_xent")
+
+
+def _here(*tensors):
+    """Every tensor on the current device, where the call's stream is."""
+    import torch
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or (t.is_cuda and t.device.index == dev), "tensors lie on the current CUDA device"
+
+
+def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bool = False, bias=None, mask=None,
+                scale: float = 0.0, status=None):
+    """mbd_expert_gemm_bf16: the products of a layer grouped by expert, the rows of expert e being offsets[e] .. offsets[e + 1]
+    (int32 [E + 1] on the GPU).
+      variant 0: A = X [T, d_in], B = W [E, d_out, d_in], out [T, d_out], bias [E, d_out] float or None, relu
+      variant 1: A = dY [T, d_out], B = W [E, d_out, d_in], out [T, d_in], op TAIL_MASK with mask [T, d_in] or None
+      variant 2: A = dY [T, d_out], B = X [T, d_in], out [E, d_out, d_in], op TAIL_SGD with scale
+    bf16 operands with free row strides (multiples of 8), `out` bf16 or float; `mask` in out's type.  Rows of `out` in no group
+    stay as they are.  `status` (int32 CUDA tensor of one zero): enqueue only; otherwise the call waits for the stream."""
+    import torch
+    _here(A, B, offsets, out, bias, mask, status)
+    assert A.dtype == torch.bfloat16 and B.dtype == torch.bfloat16 and A.dim() == 2
+    assert offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() >= 2
+    E, T = offsets.numel() - 1, A.shape[0]
+    stacked = out if variant == 2 else B                     # what has an expert dimension
+    assert variant in (0, 1, 2) and stacked.dim() == 3 and stacked.shape[0] == E
+    _, d_out, d_in = stacked.shape
+    assert A.shape[1] == (d_in if variant == 0 else d_out)
+    assert tuple(B.shape) == ((T, d_in) if variant == 2 else (E, d_out, d_in))
+    assert tuple(out.shape) == ((T, d_out), (T, d_in), (E, d_out, d_in))[variant]
+    assert bias is None or (bias.dtype == torch.float32 and tuple(bias.shape) == (E, d_out) and bias.is_contiguous())
+    assert mask is None or tuple(mask.shape) == tuple(out.shape)
+    assert _rows_in(A) and _rows_in(B) and _rows_in(out)
+    t = _tail(op, out, relu, bias, mask, scale)
+    t.ldo = _ld(out)
+    if mask is not None:
+        t.ldmask = _ld(mask)
+    _check(lib().mbd_expert_gemm_bf16(variant, E, _ptr(offsets), T, d_out, d_in, _ptr(A), _ld(A), _ptr(B), _ld(B),
+                                      stacked.stride(0), C.byref(t), _ptr(status), _stream()), "mbd_expert_gemm_bf16")
+    return out
+
+
+def _rows_in(t) -> bool:
+    return t.shape[-1] == 1 or t.stride(-1) == 1
+
+
+def _ld(t) -> int:
+    """Elements between rows.  A tensor of one row (or none) has no meaningful stride: the row rounded up to what the library asks for."""
+    return t.stride(-2) if t.shape[-2] > 1 else (t.shape[-1] + 15) // 16 * 16
+
+
+def quantize_rows(X, q, scale, sync: bool = False):
+    """mbd_quantize_rows: X [.., K] (bf16 or float; all but the last dimension are rows) to q (int8, same shape) and scale (float [..]):
+    scale = max |row| / 127, q = row / scale correctly rounded.  Enqueues only unless `sync`."""
+    import torch
+    _here(X, q, scale)
+    assert X.dtype in (torch.bfloat16, torch.float32) and q.dtype == torch.int8 and scale.dtype == torch.float32
+    assert X.dim() >= 1 and X.shape == q.shape and tuple(scale.shape) == tuple(X.shape[:-1]) and scale.is_contiguous()
+    X2, q2 = _as_rows(X), _as_rows(q)
+    _check(lib().mbd_quantize_rows(_ptr(X2), int(X.dtype == torch.bfloat16), X2.shape[0], X2.shape[1], max(X2.stride(0), X2.shape[1]),
+                                   _ptr(q2), max(q2.stride(0), q2.shape[1]), _ptr(scale), int(sync), _stream()), "mbd_quantize_rows")
+    return q, scale
+
+
+def _as_rows(t):
+    """[rows, K] view of t; t's own memory, never a copy."""
+    assert _rows_in(t)
+    return t if t.dim() == 2 else t.view(-1, t.shape[-1])
+
+
+def _i8_operands(A, a_scale, B, b_scale, out, bias, status):
+    import torch
+    _here(A, a_scale, B, b_scale, out, bias, status)
+    assert A.dtype == torch.int8 and B.dtype == torch.int8 and A.dim() == 2 and out.dim() == 2
+    assert _rows_in(A) and _rows_in(B) and _rows_in(out) and B.shape[-1] == A.shape[1]
+    assert a_scale.dtype == torch.float32 and tuple(a_scale.shape) == (A.shape[0],) and a_scale.is_contiguous()
+    assert b_scale.dtype == torch.float32 and b_scale.shape == B.shape[:-1] and b_scale.is_contiguous()
+    assert tuple(out.shape) == (A.shape[0], B.shape[-2])
+    assert bias is None or (bias.dtype == torch.float32 and bias.shape == B.shape[:-1] and bias.is_contiguous())
+
+
+def gemm_i8(A, a_scale, B, b_scale, out, relu: bool = False, bias=None, status=None):
+    """mbd_gemm_i8: out [M, N] (bf16 or float) = act(a_scale[m] b_scale[n] (A [M, K] . B [N, K]) + bias[n]) on int8 operands (row
+    strides multiples of 16).  `status`: see expert_gemm."""
+    _i8_operands(A, a_scale, B, b_scale, out, bias, status)
+    assert B.dim() == 2
+    t = _tail(TAIL_STORE, out, relu, bias)
+    t.ldo = _ld(out)
+    _check(lib().mbd_gemm_i8(A.shape[0], B.shape[0], A.shape[1], _ptr(A), _ld(A), _ptr(a_scale), _ptr(B), _ld(B),
+                             _ptr(b_scale), C.byref(t), _ptr(status), _stream()), "mbd_gemm_i8")
+    return out
+
+
+def expert_gemm_i8(A, a_scale, B, b_scale, offsets, out, relu: bool = False, bias=None, status=None):
+    """mbd_expert_gemm_i8: gemm_i8 grouped by expert: B [E, d_out, d_in], b_scale and bias [E, d_out]; rows and offsets as in
+    expert_gemm."""
+    import torch
+    _here(offsets)
+    _i8_operands(A, a_scale, B, b_scale, out, bias, status)
+    assert B.dim() == 3 and offsets.dtype == torch.int32 and offsets.is_contiguous() and tuple(offsets.shape) == (B.shape[0] + 1,)
+    t = _tail(TAIL_STORE, out, relu, bias)
+    t.ldo = _ld(out)
+    E, d_out, d_in = B.shape
+    _check(lib().mbd_expert_gemm_i8(E, _ptr(offsets), A.shape[0], d_out, d_in, _ptr(A), _ld(A), _ptr(a_scale), _ptr(B), _ld(B),
+                                    B.stride(0), _ptr(b_scale), C.byref(t), _ptr(status), _stream()), "mbd_expert_gemm_i8")
+    return out
+
+
+class AdamW:
+    """AdamW over a list of tensors, one launch per step (mbd_adamw_*, see include/mbd.h).
+    params: float or bf16 tensors; grads: their gradients (float or bf16), read at every step; masters: float copies of bf16 params
+    (or None, or None for single entries); weight_decay: a number or one per tensor.  The moments m, v (and, for state_bits = 8, the
+    scales of their blocks of 256) are allocated here as zeros unless given; state_bits = 8: float8_e4m3fn.  All tensors contiguous, on
+    the current device; the object keeps references to them."""
+
+    BLOCK = 256
+
+    def __init__(self, params, grads, masters=None, weight_decay=0.0, betas=(0.9, 0.999), eps: float = 1e-8, state_bits: int = 32,
+                 steps_done: int = 0, m=None, v=None, m_scales=None, v_scales=None):
+        import torch
+        self._h = C.c_void_p()
+        self.params, self.grads = list(params), list(grads)
+        n = len(self.params)
+        self.masters = [None] * n if masters is None else list(masters)
+        held = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+        new = lambda given, shape, dtype: list(given) if given is not None else [torch.zeros(shape(p), dtype=dtype, device=p.device) for p in self.params]  # noqa: E731
+        blocks = lambda p: ((p.numel() + self.BLOCK - 1) // self.BLOCK,)  # noqa: E731
+        self.m, self.v = new(m, lambda p: p.shape, held), new(v, lambda p: p.shape, held)
+        self.m_scales = new(m_scales, blocks, torch.float32) if state_bits == 8 else [None] * n
+        self.v_scales = new(v_scales, blocks, torch.float32) if state_bits == 8 else [None] * n
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * n
+        lists = (self.grads, self.masters, self.m, self.v, self.m_scales, self.v_scales, decay)
+        assert all(len(x) == n for x in lists)
+        table = (AdamWTensor * max(n, 1))()
+        for i, (p, g, w, a, b, sa, sb, wd) in enumerate(zip(self.params, *lists)):
+            _here(p, g, w, a, b, sa, sb)
+            assert p.dtype in (torch.float32, torch.bfloat16) and g.dtype in (torch.float32, torch.bfloat16)
+            assert all(x is None or x.is_contiguous() for x in (p, g, w, a, b, sa, sb))
+            assert g.numel() == p.numel() and a.numel() == p.numel() and b.numel() == p.numel() and a.dtype == held and b.dtype == held
+            assert w is None or (w.dtype == torch.float32 and w.numel() == p.numel())
+            assert state_bits != 8 or all(x.dtype == torch.float32 and x.numel() == blocks(p)[0] for x in (sa, sb))
+            at = lambda x: None if x is None else x.data_ptr()  # noqa: E731
+            table[i] = AdamWTensor(at(p), at(w), at(g), at(a), at(b), at(sa), at(sb), p.numel(), float(wd), int(p.dtype == torch.bfloat16),
+                                   int(g.dtype == torch.bfloat16), 0)
+        _check(lib().mbd_adamw_create(table, n, int(state_bits), float(betas[0]), float(betas[1]), float(eps), int(steps_done),
+                                      C.byref(self._h)), "mbd_adamw_create")
+
+    def step(self, lr: float, grad_scale: float = 1.0):
+        """One step on the current stream (enqueue only); grad_scale = 1 / B for gradients that are sums over a batch of B."""
+        _check(lib().mbd_adamw_step(self._h, lr, grad_scale, _stream()), "mbd_adamw_step")
+
+    @property
+    def steps_done(self) -> int:
+        """Steps taken so far, replays of captured ones included (waits for the device)."""
+        n = C.c_int64()
+        _check(lib().mbd_adamw_get_steps(self._h, C.byref(n)), "mbd_adamw_get_steps")
+        return n.value
+
+    @steps_done.setter
+    def steps_done(self, n: int):
+        _check(lib().mbd_adamw_set_steps(self._h, int(n)), "mbd_adamw_set_steps")
+
+    def close(self):
+        if self._h:
+            lib().mbd_adamw_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def selftest_timeout(limit_ms: int = 50) -> int:
