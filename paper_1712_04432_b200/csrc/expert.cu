@@ -31,7 +31,9 @@ namespace {
 using namespace tc;
 
 constexpr int MAX_EXPERTS = 512;              // bounds and tile counts of all groups are held in shared memory
-constexpr int RING_BYTES = 192 * 1024;
+constexpr int RING_BYTES = 160 * 1024;
+constexpr int BOX_BYTES = 2048, BOXES = 3;    // epilogue staging: three boxes per warp
+constexpr int SMEM_BYTES = RING_BYTES + 8 * BOXES * BOX_BYTES;
 constexpr int CH = 128;                       // channels (M side) per CTA
 constexpr int A_BYTES = CH * 128;             // one k-block is 128 bytes of every row: 64 bf16 or 128 int8
 constexpr int SEG_BLOCKS = 64;                // k-blocks per accumulation segment of a float result, see Params::seg
@@ -112,6 +114,17 @@ __device__ __forceinline__ void load_3d_pair(uint32_t dst, const CUtensorMap* tm
   asm volatile(
       "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void store_3d(const CUtensorMap* tm, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+               ::"l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
 }
 template <int KIND, int PAIR>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -313,6 +326,156 @@ __device__ __forceinline__ void finish(const Params& p, const Unit& u, const uin
   }
 }
 
+// A whole box of CNT output rows (float: 16 rows of 128 bytes, bf16: 32 rows of 64 bytes) in this warp's staging memory `box`, from
+// which one bulk store takes it: every store below is one instruction at a fixed offset, where stores to global memory row by
+// row came to 24 instructions per element of address and predicate (skewed weight gradients: 127 us).  read: the box holds what the tail
+// operation reads (the mask, or the old weights) and is combined in place.
+template <int KIND, int CNT>
+__device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const uint32_t* r, int64_t row, int lane, float bias, float ch_scale, bool read) {
+  float v[CNT];
+  if (KIND == KIND_I8) {
+    const float mine = lane < CNT ? p.row_scale[row + lane] : 0.f;
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) v[j] = static_cast<float>(static_cast<int>(r[j])) * __shfl_sync(0xffffffffu, mine, j) * ch_scale;
+  } else {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) v[j] = __uint_as_float(r[j]);
+  }
+  if (p.bias) {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) v[j] += bias;
+  }
+  if (p.relu) {
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) v[j] = relu(v[j]);
+  }
+  if (CNT == 16) {
+    float* at = reinterpret_cast<float*>(box) + lane;
+    if (read) {
+#pragma unroll
+      for (int j = 0; j < CNT; ++j) {
+        const float x = at[j * 32];
+        v[j] = p.op == EPI_SGD ? fmaf(p.scale, v[j], x) : x > 0.f ? v[j] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) at[j * 32] = v[j];
+  } else {
+    // pairs of channels: the even lane of a pair takes row 2j, the odd lane row 2j + 1
+    const int odd = lane & 1;
+    uint32_t* at = reinterpret_cast<uint32_t*>(box) + odd * 16 + (lane >> 1);
+    uint32_t w[CNT / 2];
+    if (read) {
+#pragma unroll
+      for (int j = 0; j < CNT / 2; ++j) w[j] = at[j * 32];
+    }
+#pragma unroll
+    for (int j = 0; j < CNT / 2; ++j) {
+      const float got = __shfl_xor_sync(0xffffffffu, odd ? v[2 * j] : v[2 * j + 1], 1);
+      float lo = odd ? got : v[2 * j], hi = odd ? v[2 * j + 1] : got;
+      if (read) {
+        const float xl = bf16_bits_to_f32(w[j] & 0xFFFFu), xh = bf16_bits_to_f32(w[j] >> 16);
+        if (p.op == EPI_SGD) { lo = fmaf(p.scale, lo, xl); hi = fmaf(p.scale, hi, xh); }
+        else { if (!(xl > 0.f)) lo = 0.f; if (!(xh > 0.f)) hi = 0.f; }
+      }
+      at[j * 32] = pack_bf16x2(lo, hi);
+    }
+  }
+}
+
+// The epilogue of one warp: 32 channels (a quarter of the CTA's lanes) of every second box of CNT output rows.
+template <int KIND, int B_MN, int BN, int PAIR, int CNT>
+__device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, const CUtensorMap* tmOut, const CUtensorMap* tmAux, uint8_t* boxes,
+                                         uint64_t* box_bars, uint64_t* tmem_full, uint64_t* tmem_empty, uint32_t tmem_base, int w_first, int w_step,
+                                         int total, int q, int half, int lane, uint32_t rank, volatile int* abortp) {
+  const bool read = p.op == EPI_SGD || p.mask != nullptr;
+  const CUtensorMap* src = p.op == EPI_SGD ? tmOut : tmAux;
+  int it = 0, expert = 0;
+  uint32_t n = 0, phases = 0;              // boxes so far modulo BOXES, and the parity of each box's barrier
+  bool ok = true;
+  for (int w = w_first; w < total && ok; w += w_step) {
+    const Unit u = unit_at<B_MN, BN, PAIR>(p, groups, w, expert);
+    const int m0 = u.m0 + (PAIR ? static_cast<int>(rank) * CH : 0) + q * 32, m = m0 + lane;
+    const float bias = p.bias && m < p.M ? p.bias[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
+    const float cs = KIND == KIND_I8 && m < p.M ? p.ch_scale[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
+    const int count = (u.rows + CNT - 1) / CNT;
+    const int plane = B_MN ? u.e : 0;
+    // boxes this warp moves in bulk: a group's last rows, where they do not fill a box, go element by element (the rows behind them
+    // are another group's); rows beyond an expert's gradient are cut off by the map
+    const int whole = B_MN ? count : u.rows / CNT;
+    // (a sum over segments adds to `out` element by element; a bulk store cuts rows off at multiples of 16 bytes only)
+    const bool bulk = u.kb <= p.seg && (m0 + 32 <= p.M || p.M % (CNT == 32 ? 8 : 4) == 0);
+    auto request = [&](int b, uint32_t at) {                 // lane 0
+      const uint32_t bar = smem_u32(&box_bars[at]);
+      mbar_expect_tx(bar, BOX_BYTES);
+      load_3d(smem_u32(boxes) + at * BOX_BYTES, src, m0, u.row0 + b * CNT, plane, bar);
+    };
+    if (u.kb == 0 && p.op == EPI_SGD) continue;              // an expert without rows: nothing to add to its weights
+    if (read && bulk && lane == 0) {
+      asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      if (half < whole) request(half, n);
+      if (half + 2 < whole) request(half + 2, n + 1 == BOXES ? 0 : n + 1);
+    }
+    for (int kb = 0; (kb < u.kb || kb == 0) && ok; kb += p.seg) {
+      const bool last = kb + p.seg >= u.kb, some = u.kb > 0; // an expert without rows has a gradient of zeros and no accumulator
+      const int acc = it & 1;
+      if (some) {
+        ok = mbar_wait(smem_u32(&tmem_full[acc]), (it >> 1) & 1u, abortp, p.status, DEV_TIMEOUT_EPILOGUE);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ++it;
+        tc_fence_after();
+      }
+      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * BN;
+      for (int b = half; b < count; b += 2) {
+        uint32_t r[CNT];
+        if (some) {
+          if (CNT == 32) tc_ld32(taddr + b * CNT, r);
+          else ld16(taddr + b * CNT, r);
+          tc_wait_ld();
+          if (b + 2 >= count) {                              // all of this warp's part is read: hand it back
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_cluster(in_cta(smem_u32(&tmem_empty[acc]), 0));
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < CNT; ++j) r[j] = 0;
+        }
+        if (!bulk || b >= whole) {
+          finish<KIND, CNT>(p, u, r, b * CNT, u.rows - b * CNT, m, lane, bias, cs, kb > 0, last);
+          continue;
+        }
+        uint8_t* box = boxes + n * BOX_BYTES;
+        if (read) {
+          ok = mbar_wait(smem_u32(&box_bars[n]), (phases >> n) & 1u, abortp, p.status, DEV_TIMEOUT_EPILOGUE);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          phases ^= 1u << n;
+          if (lane == 0 && b + 4 < whole) {                  // two boxes on: into the box before this one, once its store has read it
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            request(b + 4, n == 0 ? BOXES - 1 : n - 1);
+          }
+        } else if (lane == 0) {
+          asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(BOXES - 1) : "memory");
+        }
+        __syncwarp();
+        fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, lane, bias, cs, read);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) store_3d(tmOut, m0, u.row0 + b * CNT, plane, smem_u32(box));
+        if (++n == BOXES) n = 0;
+      }
+      if (some && half >= count) {                           // nothing to read for this warp
+        __syncwarp();
+        if (lane == 0) arrive_cluster(in_cta(smem_u32(&tmem_empty[acc]), 0));
+      }
+    }
+  }
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // stores done before the CTA exits
+  __syncwarp();
+}
+
 // ------------------------------------------------------------------------------------------------ the kernel
 // KIND: bf16 or int8.  A (the M side) and B (the N side) are K-major (0) or MN-major (1, bf16 only).  B_MN is variant 2:
 // K is the rows of a group.  BN: most output rows of a tile.  PAIR: two CTAs share a tile of 256 channels.  SPLIT: one unit
@@ -320,7 +483,8 @@ __device__ __forceinline__ void finish(const Params& p, const Unit& u, const uin
 template <int KIND, int A_MN, int B_MN, int BN, int PAIR, int SPLIT>
 __global__ void __launch_bounds__(B_MN ? 352 : 320, 1)
 expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                   const __grid_constant__ CUtensorMap tmB32, const Params p) {
+                   const __grid_constant__ CUtensorMap tmB32, const __grid_constant__ CUtensorMap tmOut,
+                   const __grid_constant__ CUtensorMap tmAux, const Params p) {
   constexpr int BNL = PAIR ? BN / 2 : BN;
   constexpr int STAGE_BYTES = A_BYTES + BNL * 128;
   constexpr int STAGES = RING_BYTES / STAGE_BYTES;
@@ -333,7 +497,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   __shared__ Groups groups;
   __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES];
   __shared__ __align__(8) uint64_t landed_bar[B_MN ? STAGES : 1], fixed_bar[B_MN ? STAGES : 1];
-  __shared__ __align__(8) uint64_t tmem_full_bar[2], tmem_empty_bar[2];
+  __shared__ __align__(8) uint64_t tmem_full_bar[2], tmem_empty_bar[2], box_bar[8 * BOXES];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
 
@@ -361,6 +525,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       mbar_init(smem_u32(&tmem_full_bar[i]), 1);
       mbar_init(smem_u32(&tmem_empty_bar[i]), PAIR ? 16 : 8);
     }
+    for (int i = 0; i < 8 * BOXES; ++i) mbar_init(smem_u32(&box_bar[i]), 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -505,46 +670,10 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         __syncwarp();
       }
     } else {
-      int it = 0;
-      bool ok = true;
-      for (int w = w_first; w < total && ok; w += w_step) {
-        const Unit u = unit_at<B_MN, BN, PAIR>(p, &groups, w, expert);
-        const int m = u.m0 + (PAIR ? static_cast<int>(rank) * CH : 0) + q * 32 + lane;
-        const float bias = p.bias && m < p.M ? p.bias[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
-        const float cs = KIND == KIND_I8 && m < p.M ? p.ch_scale[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
-        if (u.kb == 0) {                                   // an expert without rows: its gradient is zero
-          uint32_t r[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) r[j] = 0;
-          for (int c = half; c * 32 < u.rows; c += 2) finish<KIND, 32>(p, u, r, c * 32, u.rows - c * 32, m, lane, bias, cs, false, true);
-          continue;
-        }
-        for (int kb = 0; kb < u.kb && ok; kb += p.seg, ++it) {
-          const bool last = kb + p.seg >= u.kb;
-          const int acc = it % ACC_BUFS;
-          ok = mbar_wait(smem_u32(&tmem_full_bar[acc]), (it / ACC_BUFS) & 1u, abortp, p.status, DEV_TIMEOUT_EPILOGUE);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * BN;
-          const int chunks = (u.rows + 31) / 32;
-          for (int c = half; c < chunks; c += 2) {
-            uint32_t r[32];
-            tc_ld32(taddr + c * 32, r);
-            tc_wait_ld();
-            if (c + 2 >= chunks) {                         // all of the accumulator read: hand it back
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) arrive_cluster(in_cta(smem_u32(&tmem_empty_bar[acc]), 0));
-            }
-            finish<KIND, 32>(p, u, r, c * 32, u.rows - c * 32, m, lane, bias, cs, kb > 0, last);
-          }
-          if (half >= chunks) {                            // nothing to read for this warp
-            __syncwarp();
-            if (lane == 0) arrive_cluster(in_cta(smem_u32(&tmem_empty_bar[acc]), 0));
-          }
-        }
-      }
+      uint8_t* boxes = smem_raw + RING_BYTES + (warp - 2) * BOXES * BOX_BYTES;
+      uint64_t* bars = box_bar + (warp - 2) * BOXES;
+      if (p.out_bf16) epilogue<KIND, B_MN, BN, PAIR, 32>(p, &groups, &tmOut, &tmAux, boxes, bars, tmem_full_bar, tmem_empty_bar, tmem_base, w_first, w_step, total, q, half, lane, rank, abortp);
+      else epilogue<KIND, B_MN, BN, PAIR, 16>(p, &groups, &tmOut, &tmAux, boxes, bars, tmem_full_bar, tmem_empty_bar, tmem_base, w_first, w_step, total, q, half, lane, rank, abortp);
     }
   } else if (B_MN) {
     // ------------------------------------------------------------------ fixer
@@ -664,13 +793,13 @@ EncodeTiledFn encode_fn() {
 
 // [depth][rows][inner] with row stride `ld` and plane stride `plane` in elements of `esize` bytes; 128 bytes per box row.
 bool make_map(CUtensorMap* tm, const void* base, int esize, uint64_t inner, uint64_t rows, uint64_t depth, uint64_t ld, uint64_t plane,
-              uint32_t box_rows) {
+              uint32_t box_rows, uint32_t box_bytes = 128, bool swizzle = true) {
   const cuuint64_t dims[3] = {inner, rows, depth};
   const cuuint64_t strides[2] = {ld * esize, plane * esize};
-  const cuuint32_t box[3] = {128u / esize, box_rows, 1};
+  const cuuint32_t box[3] = {box_bytes / esize, box_rows, 1};
   const cuuint32_t estr[3] = {1, 1, 1};
-  return encode_fn()(tm, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
-                     strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  return encode_fn()(tm, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : esize == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims,
+                     strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -684,9 +813,9 @@ struct Launch {
 template <int KIND, int A_MN, int B_MN>
 cudaError_t set_attributes() {
   cudaError_t e;
-  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES)) != cudaSuccess) return e;
-  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES)) != cudaSuccess) return e;
-  return cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES);
+  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES)) != cudaSuccess) return e;
+  return cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
 }
 
 cudaError_t init(int dev) {
@@ -704,11 +833,12 @@ cudaError_t init(int dev) {
 }
 
 template <int KIND, int A_MN, int B_MN>
-cudaError_t launch(const Launch& l, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b32, const Params& p, cudaStream_t stream) {
+cudaError_t launch(const Launch& l, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b32,
+                   const CUtensorMap& out, const CUtensorMap& aux, const Params& p, cudaStream_t stream) {
   const dim3 grid(l.grid), block(B_MN ? 352 : 320);
-  if (l.pair) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, grid, block, RING_BYTES, stream, 2, a, b, b32, p);
-  if (!l.split) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, grid, block, RING_BYTES, stream, 1, a, b, b32, p);
-  return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, grid, block, RING_BYTES, stream, l.split, a, b, b32, p);
+  if (l.pair) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, grid, block, SMEM_BYTES, stream, 2, a, b, b32, out, aux, p);
+  if (!l.split) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, grid, block, SMEM_BYTES, stream, 1, a, b, b32, out, aux, p);
+  return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, grid, block, SMEM_BYTES, stream, l.split, a, b, b32, out, aux, p);
 }
 
 // Most units a call can have: a group of c rows is cut into ceil(c / BN) row tiles.
@@ -822,6 +952,14 @@ mbd_status run(Call c) {
     ok = make_map(&a, c.B, esize, c.d_in, rows, 1, c.ldb, rows * c.ldb, 64) && make_map(&b, c.A, esize, c.d_out, rows, 1, c.lda, rows * c.lda, 64);
     b32 = b;
   }
+  // results (and what the tail operation reads) in boxes of 32 channels, see fill_box
+  const int osize = t->out_bf16 ? 2 : 4;
+  const uint64_t orows = c.variant == 2 ? c.d_out : rows, odepth = c.variant == 2 ? c.E : 1;
+  CUtensorMap out, aux;
+  ok = ok && make_map(&out, t->out_dev, osize, M, orows, odepth, t->ldo, c.variant == 2 && c.E > 1 ? c.stride : orows * t->ldo, t->out_bf16 ? 32 : 16, 32 * osize, false);
+  aux = out;
+  if (t->op == MBD_TAIL_MASK && t->mask_dev)
+    ok = ok && make_map(&aux, t->mask_dev, osize, M, orows, 1, t->ldmask, orows * t->ldmask, t->out_bf16 ? 32 : 16, 32 * osize, false);
   if (!ok) return MBD_E_CUDA;
 
   Params p{};
@@ -855,10 +993,10 @@ mbd_status run(Call c) {
   }
   p.status = word;
   cudaError_t e;
-  if (c.kind == KIND_I8) e = launch<KIND_I8, 0, 0>(l, a, b, b32, p, stream);
-  else if (c.variant == 0) e = launch<KIND_BF16, 0, 0>(l, a, b, b32, p, stream);
-  else if (c.variant == 1) e = launch<KIND_BF16, 1, 0>(l, a, b, b32, p, stream);
-  else e = launch<KIND_BF16, 1, 1>(l, a, b, b32, p, stream);
+  if (c.kind == KIND_I8) e = launch<KIND_I8, 0, 0>(l, a, b, b32, out, aux, p, stream);
+  else if (c.variant == 0) e = launch<KIND_BF16, 0, 0>(l, a, b, b32, out, aux, p, stream);
+  else if (c.variant == 1) e = launch<KIND_BF16, 1, 0>(l, a, b, b32, out, aux, p, stream);
+  else e = launch<KIND_BF16, 1, 1>(l, a, b, b32, out, aux, p, stream);
   mbd_status ret = e == cudaSuccess ? MBD_OK : MBD_E_CUDA;
   if (c.status) {                          // enqueue-only: the caller owns and reads the status word
     if (ret != MBD_OK) (void)cudaGetLastError();
