@@ -47,6 +47,7 @@ struct Params {
   int kb_total;              // variants 0, 1: k-blocks
   int m_tiles, n_tiles;      // n_tiles: variant 2 only
   int group_n;               // row tiles per raster group
+  int chunked_a, chunked_b;  // MN-major operands: the map has chunks of 64 columns as a dimension, one box holds all of a tile's
   int seg;                   // k-blocks per segment: the tensor core truncates when it adds to the accumulator (relative error
                              // ~1.1e-9 per element of K, measured), so a float result is summed from segments of 4096 in
                              // full float arithmetic; a bf16 result's rounding hides it
@@ -115,6 +116,16 @@ __device__ __forceinline__ void load_3d_pair(uint32_t dst, const CUtensorMap* tm
       "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* tm, int y, int c, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(0), "r"(y), "r"(c), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void load_4d_pair(uint32_t dst, const CUtensorMap* tm, int y, int c, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(0), "r"(y), "r"(c), "r"(z), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void store_3d(const CUtensorMap* tm, int x, int y, int z, uint32_t src) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
                ::"l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
@@ -148,6 +159,10 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 }
 
 // ------------------------------------------------------------------------------------------------ work
+template <int N> struct Int { static constexpr int value = N; };
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
 struct Unit {
   int e, m0;                 // expert, first channel of the (pair's) tile
   int row0, rows;            // first output row (variant 2: within dW_e) and how many exist
@@ -491,7 +506,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   constexpr int ACC_BUFS = SPLIT ? 1 : 2;
   constexpr int TMEM_COLS = ACC_BUFS * BN;
   constexpr int ELEMS = KIND == KIND_I8 ? 128 : 64;          // elements of a k-block
-  static_assert(TMEM_COLS >= 32 && TMEM_COLS <= 512 && STAGES <= 16, "");
+  static_assert(TMEM_COLS >= 32 && TMEM_COLS <= 512 && STAGES <= 16 && (BNL == 64 || BNL == 128), "");
 
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Groups groups;
@@ -554,6 +569,10 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   auto last_kb = [&](const Unit& u) { return SPLIT ? static_cast<int>(static_cast<long long>(rank + 1) * u.kb / pieces) : u.kb; };
   // the last k-block of a group of rows holds rows of the next group, and an instruction takes 16
   auto ragged = [&](const Unit& u, int kb) { return B_MN && kb == u.kb - 1 && (u.tail & 15) != 0; };
+  // That k-block is consumed last, but takes its place in the ring (and is asked for) up to TAIL_AHEAD blocks earlier, so that
+  // clearing it is over by then: consumed where it stands it cost 1.3 us per unit.  kb1 if there is none.
+  constexpr int TAIL_AHEAD = STAGES - 2;
+  auto tail_place = [&](const Unit& u, int kb0, int kb1) { return kb1 > kb0 && ragged(u, kb1 - 1) ? max(kb0, kb1 - 1 - TAIL_AHEAD) : kb1; };
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
@@ -566,47 +585,79 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         const int m = u.m0 + (PAIR ? static_cast<int>(rank) * CH : 0);
         const int half = PAIR ? u.nt / 2 : u.nt;                      // output rows this CTA loads
         const int n = u.row0 + (PAIR ? static_cast<int>(rank) * half : 0);
-        const bool whole = half > BNL / 2;                            // one box of BNL rows, or boxes of 32
-        const int boxes = B_MN ? half / 64 : whole ? 1 : (half + 31) / 32;
-        const uint32_t bytes = A_BYTES + (B_MN ? boxes * 8192u : whole ? BNL * 128u : boxes * 4096u);
-        const int kb1 = last_kb(u);
-        for (int kb = first_kb(u); kb < kb1; ++kb) {
-          ok = mbar_wait(smem_u32(&empty_bar[stage]), phase ^ 1u, abortp, p.status, DEV_TIMEOUT_PRODUCER);
-          if (!ok) break;
+        const int kb0 = first_kb(u), kb1 = last_kb(u);
+        const int ez = B_MN ? 0 : u.e;
+        // One k-block's copies, as straight code: the issuing thread paces a tile of short boxes (with a loop over the boxes and a
+        // choice of barrier at each, the weight gradients ran at 0.97 instead of 1.1 PFLOP/s).
+        auto k_block = [&](int kb, auto clear_later, auto boxes_c, auto chunked_c) {
+          constexpr bool LATER = decltype(clear_later)::value;          // both operands' last rows will be cleared, see `fixer`
+          constexpr bool ONE_A = decltype(chunked_c)::value & 1, ONE_B = decltype(chunked_c)::value & 2;
+          constexpr int NB = decltype(boxes_c)::value;                  // boxes of the N side; K-major: 0 one box of BNL rows, else of 32
+          constexpr uint32_t BYTES = A_BYTES + (B_MN ? NB * 8192u : NB == 0 ? BNL * 128u : NB * 4096u);
           const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + A_BYTES;
-          const bool rag = ragged(u, kb);
-          const bool pair_bar = PAIR && !rag;
           uint32_t bar = smem_u32(&full_bar[stage]);
-          if (rag) {                       // each CTA of a pair learns of its own bytes; the stage is full when both have cleared it
-            if (rank == 0 || !PAIR) mbar_arrive(bar);
+          if (LATER) {                     // each CTA of a pair waits for its own bytes; nobody waits for the stage's own barrier then
+            if (!PAIR || rank == 0) mbar_arrive(bar);
             bar = smem_u32(&landed_bar[stage]);
-            mbar_expect_tx(bar, bytes);
+            mbar_expect_tx(bar, BYTES);
           } else if (!PAIR) {
-            mbar_expect_tx(bar, bytes);
+            mbar_expect_tx(bar, BYTES);
           } else {
-            if (rank == 0) mbar_expect_tx(bar, 2 * bytes);
+            if (rank == 0) mbar_expect_tx(bar, 2 * BYTES);
             bar = in_cta(bar, 0);
           }
           auto load = [&](uint32_t dst, const CUtensorMap* tm, int x, int y, int z) {
-            if (pair_bar) load_3d_pair(dst, tm, x, y, z, bar);
+            if (PAIR && !LATER) load_3d_pair(dst, tm, x, y, z, bar);
             else load_3d(dst, tm, x, y, z, bar);
           };
           const int k = B_MN ? u.k0 + kb * 64 : kb * ELEMS;
-          const int ez = B_MN ? 0 : u.e;
+          auto load_chunks = [&](uint32_t dst, const CUtensorMap* tm, int column, int row, int z) {
+            if (PAIR && !LATER) load_4d_pair(dst, tm, row, column >> 6, z, bar);
+            else load_4d(dst, tm, row, column >> 6, z, bar);
+          };
           if (A_MN == 0) {
             load(sa, &tmA, k, m, ez);
+          } else if (ONE_A) {
+            load_chunks(sa, &tmA, m, k, ez);
           } else {
 #pragma unroll
             for (int c = 0; c < CH / 64; ++c) load(sa + c * 8192, &tmA, m + c * 64, k, ez);
           }
-          if (B_MN) {
-            for (int c = 0; c < boxes; ++c) load(sb + c * 8192, &tmB, n + c * 64, k, 0);
-          } else if (whole) {
+          if (B_MN && ONE_B) {
+            load_chunks(sb, &tmB, n, k, 0);
+          } else if (B_MN) {
+#pragma unroll
+            for (int c = 0; c < NB; ++c) load(sb + c * 8192, &tmB, n + c * 64, k, 0);
+          } else if (NB == 0) {
             load(sb, &tmB, k, n, 0);
           } else {
-            for (int c = 0; c < boxes; ++c) load(sb + c * 4096, &tmB32, k, n + c * 32, 0);
+#pragma unroll
+            for (int c = 0; c < NB; ++c) load(sb + c * 4096, &tmB32, k, n + c * 32, 0);
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        };
+        auto k_blocks = [&](auto boxes_c, auto chunked_c) {
+          const int tail_at = tail_place(u, kb0, kb1);
+          for (int i = kb0; i < kb1; ++i) {
+            ok = mbar_wait(smem_u32(&empty_bar[stage]), phase ^ 1u, abortp, p.status, DEV_TIMEOUT_PRODUCER);
+            if (!ok) break;
+            if (!B_MN || i < tail_at) k_block(i, No{}, boxes_c, chunked_c);
+            else if (i == tail_at) k_block(kb1 - 1, Yes{}, boxes_c, chunked_c);
+            else k_block(i - 1, No{}, boxes_c, chunked_c);
+          }
+        };
+        auto by_rows = [&](auto chunked_c) {
+          if (half > BNL / 2) k_blocks(Int<0>{}, chunked_c);
+          else if (BNL <= 64 || half <= 32) k_blocks(Int<1>{}, chunked_c);
+          else k_blocks(Int<2>{}, chunked_c);
+        };
+        if (B_MN) {
+          if (p.chunked_a && p.chunked_b) k_blocks(Int<BNL / 64>{}, Int<3>{});
+          else k_blocks(Int<BNL / 64>{}, Int<0>{});
+        } else if (A_MN && p.chunked_a) {
+          by_rows(Int<1>{});
+        } else {
+          by_rows(Int<0>{});
         }
       }
     }
@@ -622,7 +673,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                                                 : (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(A_MN) << 15) | (uint32_t(B_MN) << 16)) |
                                (static_cast<uint32_t>(u.nt >> 3) << 17) | (uint32_t((PAIR ? 2 * CH : CH) >> 4) << 24);
         const int kb1 = last_kb(u);
-        int kb = first_kb(u);
+        int kb = first_kb(u), tail_stage = 0;
+        const int tail_at = tail_place(u, kb, kb1);
         while (kb < kb1 && ok) {                           // a segment
           const int seg_end = min(kb1, kb + p.seg);
           const int acc = it % ACC_BUFS;
@@ -633,15 +685,21 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
           const uint32_t d = tmem_base + acc * BN;
           bool add = false;
           for (; kb < seg_end; ++kb) {
-            ok = mbar_wait(smem_u32(&full_bar[stage]), phase, abortp, p.status, DEV_TIMEOUT_MMA_FULL);
-            if (!ok) break;
-            if (ragged(u, kb)) {
-              ok = wait_cluster(smem_u32(&fixed_bar[stage]), (fixed_phase >> stage) & 1u, abortp, p.status, DEV_TIMEOUT_MMA_FULL);
-              if (!ok) break;
-              fixed_phase ^= 1u << stage;
+            const bool rag = B_MN && tail_at < kb1 && kb == kb1 - 1;
+            if (B_MN && kb == tail_at) {                   // the ring's next place holds the ragged block: step over it
+              tail_stage = stage;
+              if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
+            const int at = rag ? tail_stage : stage;
+            if (rag) {
+              ok = wait_cluster(smem_u32(&fixed_bar[at]), (fixed_phase >> at) & 1u, abortp, p.status, DEV_TIMEOUT_MMA_FULL);
+              fixed_phase ^= 1u << at;
+            } else {
+              ok = mbar_wait(smem_u32(&full_bar[stage]), phase, abortp, p.status, DEV_TIMEOUT_MMA_FULL);
+            }
+            if (!ok) break;
             tc_fence_after();
-            const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + A_BYTES;
+            const uint32_t sa = ring + at * STAGE_BYTES, sb = sa + A_BYTES;
             const uint64_t ad = A_MN ? make_desc(sa, 8192, 1024) : make_desc(sa, 16, 1024);
             const uint64_t bd = B_MN ? make_desc(sb, 8192, 1024) : make_desc(sb, 16, 1024);
             constexpr uint64_t A_STEP = (A_MN ? 2048 : 32) >> 4, B_STEP = (B_MN ? 2048 : 32) >> 4;
@@ -653,8 +711,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 add = true;
               }
             }
-            commit<PAIR>(smem_u32(&empty_bar[stage]));
-            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            commit<PAIR>(smem_u32(&empty_bar[at]));
+            if (!rag && ++stage == STAGES) { stage = 0; phase ^= 1u; }
           }
           if (ok) commit<PAIR>(smem_u32(&tmem_full_bar[acc]));
         }
@@ -681,31 +739,25 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     // infinities or NaN, so multiplying them by zeros would not do: both operands' rows up to the next multiple of 16 are
     // cleared in shared memory before the instruction reads them.  A row of a swizzled chunk is 128 bytes whatever the swizzle.
     int stage = 0;
-    uint32_t landed_phase = 0;
+    uint32_t landed_phase = 0;             // one bit per stage
     bool ok = true;
     for (int w = w_first; w < total && ok; w += w_step) {
       const Unit u = unit_at<B_MN, BN, PAIR>(p, &groups, w, expert);
-      const int kb0 = first_kb(u), kb1 = last_kb(u);
-      if (kb1 > kb0) {
-        const int s = (stage + kb1 - 1 - kb0) % STAGES;
-        if (ragged(u, kb1 - 1)) {
-          ok = mbar_wait(smem_u32(&landed_bar[s]), (landed_phase >> s) & 1u, abortp, p.status, DEV_TIMEOUT_PRODUCER);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          landed_phase ^= 1u << s;
-          const int rows = ((u.tail + 15) & ~15) - u.tail;
-          const int chunks = CH / 64 + (PAIR ? u.nt / 2 : u.nt) / 64;
-          uint8_t* base = smem_raw + s * STAGE_BYTES;
-          for (int i = lane; i < chunks * rows * 8; i += 32) {
-            const int c = i / (rows * 8), v = i - c * (rows * 8);
-            *reinterpret_cast<uint4*>(base + c * 8192 + u.tail * 128 + v * 16) = make_uint4(0, 0, 0, 0);
-          }
-          asm volatile("fence.proxy.async;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) arrive_cluster(in_cta(smem_u32(&fixed_bar[s]), PAIR ? 0 : rank));
-        }
-        stage = (stage + kb1 - kb0) % STAGES;
-      }
+      const int kb0 = first_kb(u), kb1 = last_kb(u), tail_at = tail_place(u, kb0, kb1);
+      const int at = (stage + tail_at - kb0) % STAGES;
+      stage = (stage + kb1 - kb0) % STAGES;
+      if (tail_at == kb1) continue;
+      ok = mbar_wait(smem_u32(&landed_bar[at]), (landed_phase >> at) & 1u, abortp, p.status, DEV_TIMEOUT_PRODUCER);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      landed_phase ^= 1u << at;
+      const int rows = ((u.tail + 15) & ~15) - u.tail;
+      uint8_t* base = smem_raw + at * STAGE_BYTES + u.tail * 128;
+      for (int c = 0; c < CH / 64 + BNL / 64; ++c)
+        for (int v = lane; v < rows * 8; v += 32) *reinterpret_cast<uint4*>(base + c * 8192 + v * 16) = make_uint4(0, 0, 0, 0);
+      asm volatile("fence.proxy.async;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) arrive_cluster(in_cta(smem_u32(&fixed_bar[at]), PAIR ? 0 : rank));
     }
   }
 
@@ -801,6 +853,17 @@ bool make_map(CUtensorMap* tm, const void* base, int esize, uint64_t inner, uint
   return encode_fn()(tm, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : esize == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims,
                      strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The same with its columns as [chunks of 64][64]: a box holds `chunks` of them, box_rows rows each.  The width is a multiple of 64.
+bool make_chunk_map(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows, uint64_t depth, uint64_t ld, uint64_t plane,
+                    uint32_t box_rows, uint32_t chunks) {
+  const cuuint64_t dims[4] = {64, rows, inner / 64, depth};
+  const cuuint64_t strides[3] = {ld * 2, 128, plane * 2};
+  const cuuint32_t box[4] = {64, box_rows, chunks, 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return encode_fn()(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 constexpr int MAX_DEVICES = 64;
@@ -942,14 +1005,18 @@ mbd_status run(Call c) {
   const uint64_t rows = c.T > 0 ? c.T : 1;                      // (a map of no rows cannot be described; nothing is loaded then)
   CUtensorMap a, b, b32;
   bool ok;
+  int chunked_a = 0, chunked_b = 0;
   if (c.variant == 0) {
     ok = make_map(&a, c.B, esize, c.d_in, c.d_out, c.E, c.ldb, plane, CH) &&
          make_map(&b, c.A, esize, c.d_in, rows, 1, c.lda, rows * c.lda, bnl) && make_map(&b32, c.A, esize, c.d_in, rows, 1, c.lda, rows * c.lda, 32);
   } else if (c.variant == 1) {
-    ok = make_map(&a, c.B, esize, c.d_in, c.d_out, c.E, c.ldb, plane, 64) &&
+    chunked_a = c.d_in % 64 == 0;
+    ok = (chunked_a ? make_chunk_map(&a, c.B, c.d_in, c.d_out, c.E, c.ldb, plane, 64, CH / 64) : make_map(&a, c.B, esize, c.d_in, c.d_out, c.E, c.ldb, plane, 64)) &&
          make_map(&b, c.A, esize, c.d_out, rows, 1, c.lda, rows * c.lda, bnl) && make_map(&b32, c.A, esize, c.d_out, rows, 1, c.lda, rows * c.lda, 32);
   } else {
-    ok = make_map(&a, c.B, esize, c.d_in, rows, 1, c.ldb, rows * c.ldb, 64) && make_map(&b, c.A, esize, c.d_out, rows, 1, c.lda, rows * c.lda, 64);
+    chunked_a = chunked_b = c.d_in % 64 == 0 && c.d_out % 64 == 0;
+    ok = chunked_a ? make_chunk_map(&a, c.B, c.d_in, rows, 1, c.ldb, rows * c.ldb, 64, CH / 64) && make_chunk_map(&b, c.A, c.d_out, rows, 1, c.lda, rows * c.lda, 64, bnl / 64)
+                   : make_map(&a, c.B, esize, c.d_in, rows, 1, c.ldb, rows * c.ldb, 64) && make_map(&b, c.A, esize, c.d_out, rows, 1, c.lda, rows * c.lda, 64);
     b32 = b;
   }
   // results (and what the tail operation reads) in boxes of 32 channels, see fill_box
@@ -972,6 +1039,7 @@ mbd_status run(Call c) {
   p.m_tiles = static_cast<int>((M + (l.pair ? 2 * CH : CH) - 1) / (l.pair ? 2 * CH : CH));
   p.n_tiles = static_cast<int>((N + l.BN - 1) / l.BN);
   p.group_n = 8;
+  p.chunked_a = chunked_a; p.chunked_b = chunked_b;
   p.seg = c.kind == KIND_BF16 && !t->out_bf16 && !l.split ? SEG_BLOCKS : 1 << 30;
   p.op = t->op == MBD_TAIL_STORE ? EPI_ACT : t->op == MBD_TAIL_MASK ? EPI_MASK : EPI_SGD;
   p.out_bf16 = t->out_bf16 != 0;
