@@ -19,7 +19,7 @@
 // The split form cuts K over the CTAs of a cluster and joins the pieces through distributed shared memory, for calls
 // with too few tiles to keep the SMs busy.
 // Every wait is bounded; on time-out the kernel records a code and leaves.
-#include <stdlib.h>
+#include <atomic>
 
 #include "../../include/mbd.h"
 #include "epi.cuh"
@@ -881,18 +881,20 @@ cudaError_t set_attributes() {
   return cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
 }
 
-cudaError_t init(int dev) {
-  static bool done[MAX_DEVICES] = {false};       // the opt-in to large shared memory is per device; setting it twice does no harm
-  if (dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
-  if (done[dev]) return cudaSuccess;
-  if (!encode_fn()) return cudaErrorNotSupported;
-  cudaError_t e;
-  if ((e = set_attributes<KIND_BF16, 0, 0>()) != cudaSuccess) return e;
-  if ((e = set_attributes<KIND_BF16, 1, 0>()) != cudaSuccess) return e;
-  if ((e = set_attributes<KIND_BF16, 1, 1>()) != cudaSuccess) return e;
-  if ((e = set_attributes<KIND_I8, 0, 0>()) != cudaSuccess) return e;
-  done[dev] = true;
-  return cudaSuccess;
+// What a device needs before its first launch, and how many SMs it has.  (The opt-in to large shared memory is per device; two threads
+// that come here at once set the same values.)
+mbd_status ready(int dev, int* sms) {
+  static std::atomic<int> known[MAX_DEVICES];
+  if (dev < 0 || dev >= MAX_DEVICES) return MBD_E_UNSUPPORTED;
+  if ((*sms = known[dev].load(std::memory_order_acquire)) > 0) return MBD_OK;
+  int major = 0;
+  if (cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return MBD_E_CUDA;
+  if (major != 10) return MBD_E_UNSUPPORTED;
+  if (!encode_fn() || set_attributes<KIND_BF16, 0, 0>() != cudaSuccess || set_attributes<KIND_BF16, 1, 0>() != cudaSuccess ||
+      set_attributes<KIND_BF16, 1, 1>() != cudaSuccess || set_attributes<KIND_I8, 0, 0>() != cudaSuccess) return MBD_E_CUDA;
+  known[dev].store(*sms, std::memory_order_release);
+  return MBD_OK;
 }
 
 template <int KIND, int A_MN, int B_MN>
@@ -987,18 +989,15 @@ mbd_status run(Call c) {
   if (c.variant == 2 ? static_cast<double>(c.E) * mt * ((N + 63) / 64) > 1e9 : static_cast<double>(mt) * (c.T / 64 + groups + 1) > 1e9) return MBD_E_UNSUPPORTED;
   if (c.T == 0 && c.variant != 2) return MBD_OK;                // no rows, nothing to write
 
-  int dev = 0, sms = 0, major = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return MBD_E_CUDA;
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_CUDA; }
+  {
+    const mbd_status st = ready(dev, &sms);
+    if (st != MBD_OK) { (void)cudaGetLastError(); return st; }
   }
-  if (major != 10) return MBD_E_UNSUPPORTED;
-  if (init(dev) != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_CUDA; }
   cudaStream_t stream = static_cast<cudaStream_t>(c.stream);
 
-  Launch l = plan(c.kind, c.variant, c.E, c.T, M, N, c.d_in, !t->out_bf16, sms);
-  if (c.variant == 1) l = plan(c.kind, 1, c.E, c.T, M, N, c.d_out, !t->out_bf16, sms);
+  const Launch l = plan(c.kind, c.variant, c.E, c.T, M, N, c.variant == 1 ? c.d_out : c.d_in, !t->out_bf16, sms);
   const int bnl = l.pair ? l.BN / 2 : l.BN;
   const int esize = c.kind == KIND_I8 ? 1 : 2;
   const uint64_t plane = c.E > 1 ? static_cast<uint64_t>(c.stride) : static_cast<uint64_t>(c.d_out) * c.ldb;

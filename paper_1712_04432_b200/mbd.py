@@ -548,12 +548,42 @@ def softmax_xent(logits, labels, dY, per_sample, sync: bool = True):
                                   _ptr(per_sample), int(sync), _stream()), "mbd_softmax_xent")
 
 
-def _here(*tensors):
-    """Every tensor on the current device, where the call's stream is."""
+def _at(t, dev: int) -> int:
+    """Address of a tensor on the current device, where the call's stream is."""
+    assert t.get_device() == dev, "tensors lie on the current CUDA device"
+    return t.data_ptr()
+
+
+def _at_or_none(t, dev: int):
+    return None if t is None else _at(t, dev)
+
+
+def _ld(t, shape, stride) -> int:
+    """Elements between rows.  A tensor of one row (or none) has no meaningful stride: the row rounded up to what the library asks for."""
+    assert stride[-1] == 1 or shape[-1] == 1
+    return stride[-2] if shape[-2] > 1 else (shape[-1] + 15) // 16 * 16
+
+
+def _group_tail(op: int, out, out_shape, dev: int, relu: bool, bias, bias_shape, mask, scale: float) -> Tail:
+    import torch
+    dt = out.dtype
+    assert dt in (torch.bfloat16, torch.float32) and out.shape == out_shape
+    t = Tail(op, dt == torch.bfloat16, relu, 0, _at(out, dev), _ld(out, out_shape, out.stride()), None, None, 0, scale)
+    if bias is not None:
+        assert bias.dtype == torch.float32 and bias.shape == bias_shape and bias.is_contiguous()
+        t.bias_dev = _at(bias, dev)
+    if mask is not None:
+        assert mask.dtype == dt and mask.shape == out_shape
+        t.mask_dev = _at(mask, dev)
+        t.ldmask = _ld(mask, out_shape, mask.stride())
+    return t
+
+
+def _device():
+    """The current device and its current stream."""
     import torch
     dev = torch.cuda.current_device()
-    for t in tensors:
-        assert t is None or (t.is_cuda and t.device.index == dev), "tensors lie on the current CUDA device"
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
 
 
 def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bool = False, bias=None, mask=None,
@@ -566,76 +596,71 @@ def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bo
     bf16 operands with free row strides (multiples of 8), `out` bf16 or float; `mask` in out's type.  Rows of `out` in no group
     stay as they are.  `status` (int32 CUDA tensor of one zero): enqueue only; otherwise the call waits for the stream."""
     import torch
-    _here(A, B, offsets, out, bias, mask, status)
-    assert A.dtype == torch.bfloat16 and B.dtype == torch.bfloat16 and A.dim() == 2
-    assert offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() >= 2
-    E, T = offsets.numel() - 1, A.shape[0]
-    stacked = out if variant == 2 else B                     # what has an expert dimension
-    assert variant in (0, 1, 2) and stacked.dim() == 3 and stacked.shape[0] == E
-    _, d_out, d_in = stacked.shape
-    assert A.shape[1] == (d_in if variant == 0 else d_out)
-    assert tuple(B.shape) == ((T, d_in) if variant == 2 else (E, d_out, d_in))
-    assert tuple(out.shape) == ((T, d_out), (T, d_in), (E, d_out, d_in))[variant]
-    assert bias is None or (bias.dtype == torch.float32 and tuple(bias.shape) == (E, d_out) and bias.is_contiguous())
-    assert mask is None or tuple(mask.shape) == tuple(out.shape)
-    assert _rows_in(A) and _rows_in(B) and _rows_in(out)
-    t = _tail(op, out, relu, bias, mask, scale)
-    t.ldo = _ld(out)
-    if mask is not None:
-        t.ldmask = _ld(mask)
-    _check(lib().mbd_expert_gemm_bf16(variant, E, _ptr(offsets), T, d_out, d_in, _ptr(A), _ld(A), _ptr(B), _ld(B),
-                                      stacked.stride(0), C.byref(t), _ptr(status), _stream()), "mbd_expert_gemm_bf16")
+    dev, stream = _device()
+    sa, sb, so = A.shape, B.shape, offsets.shape
+    assert A.dtype == torch.bfloat16 and B.dtype == torch.bfloat16 and offsets.dtype == torch.int32
+    assert len(sa) == 2 and len(so) == 1 and so[0] >= 2 and (so[0] == 2 or offsets.stride(0) == 1)
+    E, T = so[0] - 1, sa[0]
+    if variant == 2:
+        assert len(sb) == 2 and sb[0] == T
+        d_out, d_in = sa[1], sb[1]
+        shape, stacked = (E, d_out, d_in), out
+    else:
+        assert variant in (0, 1) and len(sb) == 3 and sb[0] == E
+        _, d_out, d_in = sb
+        assert sa[1] == (d_out if variant else d_in)
+        shape, stacked = (T, d_in if variant else d_out), B
+    t = _group_tail(op, out, shape, dev, relu, bias, (E, d_out), mask, scale)
+    _check(lib().mbd_expert_gemm_bf16(variant, E, _at(offsets, dev), T, d_out, d_in, _at(A, dev), _ld(A, sa, A.stride()), _at(B, dev),
+                                      _ld(B, sb, B.stride()), stacked.stride(0), C.byref(t), _at_or_none(status, dev), stream),
+           "mbd_expert_gemm_bf16")
     return out
-
-
-def _rows_in(t) -> bool:
-    return t.shape[-1] == 1 or t.stride(-1) == 1
-
-
-def _ld(t) -> int:
-    """Elements between rows.  A tensor of one row (or none) has no meaningful stride: the row rounded up to what the library asks for."""
-    return t.stride(-2) if t.shape[-2] > 1 else (t.shape[-1] + 15) // 16 * 16
 
 
 def quantize_rows(X, q, scale, sync: bool = False):
     """mbd_quantize_rows: X [.., K] (bf16 or float; all but the last dimension are rows) to q (int8, same shape) and scale (float [..]):
     scale = max |row| / 127, q = row / scale correctly rounded.  Enqueues only unless `sync`."""
     import torch
-    _here(X, q, scale)
+    dev, stream = _device()
+    shape = X.shape
     assert X.dtype in (torch.bfloat16, torch.float32) and q.dtype == torch.int8 and scale.dtype == torch.float32
-    assert X.dim() >= 1 and X.shape == q.shape and tuple(scale.shape) == tuple(X.shape[:-1]) and scale.is_contiguous()
-    X2, q2 = _as_rows(X), _as_rows(q)
-    _check(lib().mbd_quantize_rows(_ptr(X2), int(X.dtype == torch.bfloat16), X2.shape[0], X2.shape[1], max(X2.stride(0), X2.shape[1]),
-                                   _ptr(q2), max(q2.stride(0), q2.shape[1]), _ptr(scale), int(sync), _stream()), "mbd_quantize_rows")
+    assert len(shape) >= 1 and q.shape == shape and scale.shape == shape[:-1] and scale.is_contiguous()
+    (rows, K), ldx = _as_rows(X, shape)
+    _, ldq = _as_rows(q, shape)
+    _check(lib().mbd_quantize_rows(_at(X, dev), X.dtype == torch.bfloat16, rows, K, ldx, _at(q, dev), ldq, _at(scale, dev), sync, stream),
+           "mbd_quantize_rows")
     return q, scale
 
 
-def _as_rows(t):
-    """[rows, K] view of t; t's own memory, never a copy."""
-    assert _rows_in(t)
-    return t if t.dim() == 2 else t.view(-1, t.shape[-1])
+def _as_rows(t, shape):
+    """((rows, K), row stride) of t seen as [rows, K]; its own memory, never a copy."""
+    if len(shape) != 2:
+        t = t.view(-1, shape[-1])
+        shape = t.shape
+    rows, K = shape
+    stride = t.stride()
+    assert K == 1 or stride[1] == 1
+    return (rows, K), (max(stride[0], K) if rows > 1 else K)
 
 
-def _i8_operands(A, a_scale, B, b_scale, out, bias, status):
+def _i8(A, a_scale, B, b_scale, out, relu, bias, dev):
     import torch
-    _here(A, a_scale, B, b_scale, out, bias, status)
-    assert A.dtype == torch.int8 and B.dtype == torch.int8 and A.dim() == 2 and out.dim() == 2
-    assert _rows_in(A) and _rows_in(B) and _rows_in(out) and B.shape[-1] == A.shape[1]
-    assert a_scale.dtype == torch.float32 and tuple(a_scale.shape) == (A.shape[0],) and a_scale.is_contiguous()
-    assert b_scale.dtype == torch.float32 and b_scale.shape == B.shape[:-1] and b_scale.is_contiguous()
-    assert tuple(out.shape) == (A.shape[0], B.shape[-2])
-    assert bias is None or (bias.dtype == torch.float32 and bias.shape == B.shape[:-1] and bias.is_contiguous())
+    sa, sb = A.shape, B.shape
+    assert A.dtype == torch.int8 and B.dtype == torch.int8 and len(sa) == 2 and sb[-1] == sa[1]
+    assert a_scale.dtype == torch.float32 and a_scale.shape == sa[:1] and a_scale.is_contiguous()
+    assert b_scale.dtype == torch.float32 and b_scale.shape == sb[:-1] and b_scale.is_contiguous()
+    t = _group_tail(TAIL_STORE, out, (sa[0], sb[-2]), dev, relu, bias, sb[:-1], None, 0.0)
+    return sa, sb, _ld(A, sa, A.stride()), _ld(B, sb, B.stride()), t
 
 
 def gemm_i8(A, a_scale, B, b_scale, out, relu: bool = False, bias=None, status=None):
     """mbd_gemm_i8: out [M, N] (bf16 or float) = act(a_scale[m] b_scale[n] (A [M, K] . B [N, K]) + bias[n]) on int8 operands (row
     strides multiples of 16).  `status`: see expert_gemm."""
-    _i8_operands(A, a_scale, B, b_scale, out, bias, status)
-    assert B.dim() == 2
-    t = _tail(TAIL_STORE, out, relu, bias)
-    t.ldo = _ld(out)
-    _check(lib().mbd_gemm_i8(A.shape[0], B.shape[0], A.shape[1], _ptr(A), _ld(A), _ptr(a_scale), _ptr(B), _ld(B),
-                             _ptr(b_scale), C.byref(t), _ptr(status), _stream()), "mbd_gemm_i8")
+    dev, stream = _device()
+    sa, sb, lda, ldb, t = _i8(A, a_scale, B, b_scale, out, relu, bias, dev)
+    assert len(sb) == 2
+    _check(lib().mbd_gemm_i8(sa[0], sb[0], sa[1], _at(A, dev), lda, _at(a_scale, dev), _at(B, dev), ldb, _at(b_scale, dev), C.byref(t),
+                             _at_or_none(status, dev), stream), "mbd_gemm_i8")
     return out
 
 
@@ -643,14 +668,11 @@ def expert_gemm_i8(A, a_scale, B, b_scale, offsets, out, relu: bool = False, bia
     """mbd_expert_gemm_i8: gemm_i8 grouped by expert: B [E, d_out, d_in], b_scale and bias [E, d_out]; rows and offsets as in
     expert_gemm."""
     import torch
-    _here(offsets)
-    _i8_operands(A, a_scale, B, b_scale, out, bias, status)
-    assert B.dim() == 3 and offsets.dtype == torch.int32 and offsets.is_contiguous() and tuple(offsets.shape) == (B.shape[0] + 1,)
-    t = _tail(TAIL_STORE, out, relu, bias)
-    t.ldo = _ld(out)
-    E, d_out, d_in = B.shape
-    _check(lib().mbd_expert_gemm_i8(E, _ptr(offsets), A.shape[0], d_out, d_in, _ptr(A), _ld(A), _ptr(a_scale), _ptr(B), _ld(B),
-                                    B.stride(0), _ptr(b_scale), C.byref(t), _ptr(status), _stream()), "mbd_expert_gemm_i8")
+    dev, stream = _device()
+    sa, sb, lda, ldb, t = _i8(A, a_scale, B, b_scale, out, relu, bias, dev)
+    assert len(sb) == 3 and offsets.dtype == torch.int32 and offsets.is_contiguous() and offsets.shape == (sb[0] + 1,)
+    _check(lib().mbd_expert_gemm_i8(sb[0], _at(offsets, dev), sa[0], sb[1], sb[2], _at(A, dev), lda, _at(a_scale, dev), _at(B, dev), ldb,
+                                    B.stride(0), _at(b_scale, dev), C.byref(t), _at_or_none(status, dev), stream), "mbd_expert_gemm_i8")
     return out
 
 
@@ -680,14 +702,14 @@ class AdamW:
         lists = (self.grads, self.masters, self.m, self.v, self.m_scales, self.v_scales, decay)
         assert all(len(x) == n for x in lists)
         table = (AdamWTensor * max(n, 1))()
+        dev = torch.cuda.current_device()
+        at = lambda x: _at_or_none(x, dev)  # noqa: E731
         for i, (p, g, w, a, b, sa, sb, wd) in enumerate(zip(self.params, *lists)):
-            _here(p, g, w, a, b, sa, sb)
             assert p.dtype in (torch.float32, torch.bfloat16) and g.dtype in (torch.float32, torch.bfloat16)
             assert all(x is None or x.is_contiguous() for x in (p, g, w, a, b, sa, sb))
             assert g.numel() == p.numel() and a.numel() == p.numel() and b.numel() == p.numel() and a.dtype == held and b.dtype == held
             assert w is None or (w.dtype == torch.float32 and w.numel() == p.numel())
             assert state_bits != 8 or all(x.dtype == torch.float32 and x.numel() == blocks(p)[0] for x in (sa, sb))
-            at = lambda x: None if x is None else x.data_ptr()  # noqa: E731
             table[i] = AdamWTensor(at(p), at(w), at(g), at(a), at(b), at(sa), at(sb), p.numel(), float(wd), int(p.dtype == torch.bfloat16),
                                    int(g.dtype == torch.bfloat16), 0)
         _check(lib().mbd_adamw_create(table, n, int(state_bits), float(betas[0]), float(betas[1]), float(eps), int(steps_done),
@@ -695,7 +717,7 @@ class AdamW:
 
     def step(self, lr: float, grad_scale: float = 1.0):
         """One step on the current stream (enqueue only); grad_scale = 1 / B for gradients that are sums over a batch of B."""
-        _check(lib().mbd_adamw_step(self._h, lr, grad_scale, _stream()), "mbd_adamw_step")
+        _check(lib().mbd_adamw_step(self._h, lr, grad_scale, _device()[1]), "mbd_adamw_step")
 
     @property
     def steps_done(self) -> int:

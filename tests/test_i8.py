@@ -58,7 +58,8 @@ def _want_rows(X):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("R,K", [(1, 1), (1, 7), (3, 8), (5, 33), (2, 1001), (700, 64), (300, 1032), (4, 9216), (2, 32768), (1, 40007), (400, 8200)])
+@pytest.mark.parametrize("R,K", [(1, 1), (1, 7), (3, 8), (5, 33), (2, 1001), (700, 64), (300, 1032), (4, 9216), (2, 32768), (1, 40007), (400, 8200),
+                                 (700, 8192), (3000, 24), (601, 1003), (1300, 2056), (650, 16384), (2000, 8)])
 def test_rows(R, K, dtype):
     import torch
     gen = torch.Generator(device="cuda")
