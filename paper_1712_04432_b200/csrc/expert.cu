@@ -341,15 +341,16 @@ __device__ __forceinline__ void finish(const Params& p, const Unit& u, const uin
   }
 }
 
-// A whole box of CNT output rows (float: 16 rows of 128 bytes, bf16: 32 rows of 64 bytes) in this warp's staging memory `box`, from
-// which one bulk store takes it: every store below is one instruction at a fixed offset, where stores to global memory row by
-// row came to 24 instructions per element of address and predicate (skewed weight gradients: 127 us).  read: the box holds what the tail
-// operation reads (the mask, or the old weights) and is combined in place.
+// A box of CNT output rows of this warp's 32 channels (float: 16 rows of 128 bytes, bf16: 32 rows of 64 bytes) in staging memory: turned
+// from a channel per lane to rows, so that 16 bytes of a row can leave (and 16 bytes of a mask be met) per lane.  Going to global memory
+// straight from the accumulator's layout cost 24 instructions per element of address and predicate (skewed weight gradients 127
+// against 85 us).  read: the box holds the old weights of
+// Eq. 1 and is combined in place.
 template <int KIND, int CNT>
-__device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const uint32_t* r, int64_t row, int lane, float bias, float ch_scale, bool read) {
+__device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const uint32_t* r, int64_t row, int rows, int lane, float bias, float ch_scale, bool read) {
   float v[CNT];
   if (KIND == KIND_I8) {
-    const float mine = lane < CNT ? p.row_scale[row + lane] : 0.f;
+    const float mine = lane < rows ? p.row_scale[row + lane] : 0.f;
 #pragma unroll
     for (int j = 0; j < CNT; ++j) v[j] = static_cast<float>(static_cast<int>(r[j])) * __shfl_sync(0xffffffffu, mine, j) * ch_scale;
   } else {
@@ -368,10 +369,7 @@ __device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const ui
     float* at = reinterpret_cast<float*>(box) + lane;
     if (read) {
 #pragma unroll
-      for (int j = 0; j < CNT; ++j) {
-        const float x = at[j * 32];
-        v[j] = p.op == EPI_SGD ? fmaf(p.scale, v[j], x) : x > 0.f ? v[j] : 0.f;
-      }
+      for (int j = 0; j < CNT; ++j) v[j] = fmaf(p.scale, v[j], at[j * 32]);
     }
 #pragma unroll
     for (int j = 0; j < CNT; ++j) at[j * 32] = v[j];
@@ -390,23 +388,34 @@ __device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const ui
       float lo = odd ? got : v[2 * j], hi = odd ? v[2 * j + 1] : got;
       if (read) {
         const float xl = bf16_bits_to_f32(w[j] & 0xFFFFu), xh = bf16_bits_to_f32(w[j] >> 16);
-        if (p.op == EPI_SGD) { lo = fmaf(p.scale, lo, xl); hi = fmaf(p.scale, hi, xh); }
-        else { if (!(xl > 0.f)) lo = 0.f; if (!(xh > 0.f)) hi = 0.f; }
+        lo = fmaf(p.scale, lo, xl);
+        hi = fmaf(p.scale, hi, xh);
       }
       at[j * 32] = pack_bf16x2(lo, hi);
     }
   }
 }
 
+// 16 bytes of results, where the mask (of the same place) is positive.
+template <int CNT>
+__device__ __forceinline__ uint4 masked(const uint4& v, const uint4& mask) {
+  const auto keep = [](uint32_t x, uint32_t m) {
+    if (CNT == 16) return __uint_as_float(m) > 0.f ? x : 0u;
+    const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
+    return x & __hgt2_mask(*reinterpret_cast<const __nv_bfloat162*>(&m), zero);
+  };
+  return make_uint4(keep(v.x, mask.x), keep(v.y, mask.y), keep(v.z, mask.z), keep(v.w, mask.w));
+}
+
 // The epilogue of one warp: 32 channels (a quarter of the CTA's lanes) of every second box of CNT output rows.
 template <int KIND, int B_MN, int BN, int PAIR, int CNT>
-__device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, const CUtensorMap* tmOut, const CUtensorMap* tmAux, uint8_t* boxes,
-                                         uint64_t* box_bars, uint64_t* tmem_full, uint64_t* tmem_empty, uint32_t tmem_base, int w_first, int w_step,
-                                         int total, int q, int half, int lane, uint32_t rank, volatile int* abortp) {
-  const bool read = p.op == EPI_SGD || p.mask != nullptr;
-  const CUtensorMap* src = p.op == EPI_SGD ? tmOut : tmAux;
+__device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, const CUtensorMap* tmOut, uint8_t* boxes, uint64_t* box_bars,
+                                         uint64_t* tmem_full, uint64_t* tmem_empty, uint32_t tmem_base, int w_first, int w_step, int total,
+                                         int q, int half, int lane, uint32_t rank, volatile int* abortp) {
+  constexpr int SIZE = CNT == 32 ? 2 : 4, LANES = 32 * SIZE / 16, ROWS = 32 / LANES;      // lanes per row, rows per access
+  const bool sgd = p.op == EPI_SGD, mask = p.op == EPI_MASK && p.mask != nullptr;
   int it = 0, expert = 0;
-  uint32_t n = 0, phases = 0;              // boxes so far modulo BOXES, and the parity of each box's barrier
+  uint32_t n = 0, phases = 0;              // SGD: boxes so far modulo BOXES, and the parity of each box's barrier
   bool ok = true;
   for (int w = w_first; w < total && ok; w += w_step) {
     const Unit u = unit_at<B_MN, BN, PAIR>(p, groups, w, expert);
@@ -414,23 +423,35 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
     const float bias = p.bias && m < p.M ? p.bias[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
     const float cs = KIND == KIND_I8 && m < p.M ? p.ch_scale[static_cast<int64_t>(u.e) * p.M + m] : 0.f;
     const int count = (u.rows + CNT - 1) / CNT;
+    // element by element: a sum over segments (it adds to `out`), and an edge that cuts 16 bytes in two
+    const bool staged = u.kb <= p.seg && (m0 + 32 <= p.M || p.M % (16 / SIZE) == 0);
     const int plane = B_MN ? u.e : 0;
-    // boxes this warp moves in bulk: a group's last rows, where they do not fill a box, go element by element (the rows behind them
-    // are another group's); rows beyond an expert's gradient are cut off by the map
-    const int whole = B_MN ? count : u.rows / CNT;
-    // (a sum over segments adds to `out` element by element; a bulk store cuts rows off at multiples of 16 bytes only)
-    const bool bulk = u.kb <= p.seg && (m0 + 32 <= p.M || p.M % (CNT == 32 ? 8 : 4) == 0);
+    if (u.kb == 0 && sgd) continue;                          // an expert without rows: nothing to add to its weights
+    // this lane's 16 bytes of a box's first rows
+    const int ch = m0 + lane % LANES * (16 / SIZE), lr = lane / LANES;
+    const bool column = ch < p.M;
+    char* const out = reinterpret_cast<char*>(p.out) + (u.e * p.out_stride + (u.row0 + lr) * p.ldo + ch) * SIZE;
+    const char* const mask_at = reinterpret_cast<const char*>(p.mask) + ((u.row0 + lr) * p.ldmask + ch) * SIZE;
+    uint4 mk[4];
+    auto load_mask = [&](int b) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = b * CNT + i * ROWS;
+        mk[i] = column && row + lr < u.rows ? *reinterpret_cast<const uint4*>(mask_at + row * p.ldmask * SIZE) : make_uint4(0, 0, 0, 0);
+      }
+    };
+    // the old weights arrive by bulk copies
     auto request = [&](int b, uint32_t at) {                 // lane 0
       const uint32_t bar = smem_u32(&box_bars[at]);
       mbar_expect_tx(bar, BOX_BYTES);
-      load_3d(smem_u32(boxes) + at * BOX_BYTES, src, m0, u.row0 + b * CNT, plane, bar);
+      load_3d(smem_u32(boxes) + at * BOX_BYTES, tmOut, m0, u.row0 + b * CNT, u.e, bar);
     };
-    if (u.kb == 0 && p.op == EPI_SGD) continue;              // an expert without rows: nothing to add to its weights
-    if (read && bulk && lane == 0) {
+    if (sgd && staged && lane == 0) {
       asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-      if (half < whole) request(half, n);
-      if (half + 2 < whole) request(half + 2, n + 1 == BOXES ? 0 : n + 1);
+      if (half < count) request(half, n);
+      if (half + 2 < count) request(half + 2, n + 1 == BOXES ? 0 : n + 1);
     }
+    if (mask && staged && half < count) load_mask(half);     // its latency passes under the tile's products
     for (int kb = 0; (kb < u.kb || kb == 0) && ok; kb += p.seg) {
       const bool last = kb + p.seg >= u.kb, some = u.kb > 0; // an expert without rows has a gradient of zeros and no accumulator
       const int acc = it & 1;
@@ -457,28 +478,56 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
 #pragma unroll
           for (int j = 0; j < CNT; ++j) r[j] = 0;
         }
-        if (!bulk || b >= whole) {
-          finish<KIND, CNT>(p, u, r, b * CNT, u.rows - b * CNT, m, lane, bias, cs, kb > 0, last);
+        const int left = u.rows - b * CNT;
+        if (!staged) {
+          finish<KIND, CNT>(p, u, r, b * CNT, left, m, lane, bias, cs, kb > 0, last);
           continue;
         }
         uint8_t* box = boxes + n * BOX_BYTES;
-        if (read) {
+        if (sgd) {                                           // (only for an expert's weights: rows beyond them are cut off by the map)
           ok = mbar_wait(smem_u32(&box_bars[n]), (phases >> n) & 1u, abortp, p.status, DEV_TIMEOUT_EPILOGUE);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           phases ^= 1u << n;
-          if (lane == 0 && b + 4 < whole) {                  // two boxes on: into the box before this one, once its store has read it
-            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            request(b + 4, n == 0 ? BOXES - 1 : n - 1);
+          fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, left, lane, bias, cs, true);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            store_3d(tmOut, m0, u.row0 + b * CNT, u.e, smem_u32(box));
+            if (b + 4 < count) {                             // two boxes on: into the box before this one, once its store has read it
+              asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+              request(b + 4, n == 0 ? BOXES - 1 : n - 1);
+            }
           }
-        } else if (lane == 0) {
-          asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(BOXES - 1) : "memory");
+        } else {
+          // by one bulk store where the whole box is this group's; with a mask, or at a group's last rows (those behind them are another
+          // group's), by 16 bytes a lane.  (All boxes that way: weight gradients 282 against 251 us, the stores share the issue slots of
+          // the warps.  Masks by bulk copies: backward-data 80 against 73 us, they queue behind the operands' copies.)
+          const bool bulk = !mask && (B_MN || left >= CNT);
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(BOXES - 1) : "memory");      // the store that used this box has read it
+          __syncwarp();
+          fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, left, lane, bias, cs, false);
+          if (bulk) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) store_3d(tmOut, m0, u.row0 + b * CNT, plane, smem_u32(box));
+          } else {
+            if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");      // (a group of its own, so that the count above holds)
+            __syncwarp();
+            uint4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint4*>(box + i * 512 + lane * 16);
+            if (mask) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) v[i] = masked<CNT>(v[i], mk[i]);
+              if (b + 2 < count) load_mask(b + 2);
+            }
+            char* at = out + b * CNT * p.ldo * SIZE;
+#pragma unroll
+            for (int i = 0; i < 4; ++i, at += ROWS * p.ldo * SIZE)
+              if (column && lr + i * ROWS < left) *reinterpret_cast<uint4*>(at) = v[i];
+          }
         }
-        __syncwarp();
-        fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, lane, bias, cs, read);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) store_3d(tmOut, m0, u.row0 + b * CNT, plane, smem_u32(box));
         if (++n == BOXES) n = 0;
       }
       if (some && half >= count) {                           // nothing to read for this warp
@@ -499,7 +548,7 @@ template <int KIND, int A_MN, int B_MN, int BN, int PAIR, int SPLIT>
 __global__ void __launch_bounds__(B_MN ? 352 : 320, 1)
 expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmB32, const __grid_constant__ CUtensorMap tmOut,
-                   const __grid_constant__ CUtensorMap tmAux, const Params p) {
+                   const Params p) {
   constexpr int BNL = PAIR ? BN / 2 : BN;
   constexpr int STAGE_BYTES = A_BYTES + BNL * 128;
   constexpr int STAGES = RING_BYTES / STAGE_BYTES;
@@ -647,9 +696,10 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
           }
         };
         auto by_rows = [&](auto chunked_c) {
-          if (half > BNL / 2) k_blocks(Int<0>{}, chunked_c);
+          if (half > BNL - 32) k_blocks(Int<0>{}, chunked_c);
           else if (BNL <= 64 || half <= 32) k_blocks(Int<1>{}, chunked_c);
-          else k_blocks(Int<2>{}, chunked_c);
+          else if (half <= 64) k_blocks(Int<2>{}, chunked_c);
+          else k_blocks(Int<3>{}, chunked_c);
         };
         if (B_MN) {
           if (p.chunked_a && p.chunked_b) k_blocks(Int<BNL / 64>{}, Int<3>{});
@@ -730,8 +780,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     } else {
       uint8_t* boxes = smem_raw + RING_BYTES + (warp - 2) * BOXES * BOX_BYTES;
       uint64_t* bars = box_bar + (warp - 2) * BOXES;
-      if (p.out_bf16) epilogue<KIND, B_MN, BN, PAIR, 32>(p, &groups, &tmOut, &tmAux, boxes, bars, tmem_full_bar, tmem_empty_bar, tmem_base, w_first, w_step, total, q, half, lane, rank, abortp);
-      else epilogue<KIND, B_MN, BN, PAIR, 16>(p, &groups, &tmOut, &tmAux, boxes, bars, tmem_full_bar, tmem_empty_bar, tmem_base, w_first, w_step, total, q, half, lane, rank, abortp);
+      if (p.out_bf16) epilogue<KIND, B_MN, BN, PAIR, 32>(p, &groups, &tmOut, boxes, bars, tmem_full_bar, tmem_empty_bar, tmem_base, w_first, w_step, total, q, half, lane, rank, abortp);
+      else epilogue<KIND, B_MN, BN, PAIR, 16>(p, &groups, &tmOut, boxes, bars, tmem_full_bar, tmem_empty_bar, tmem_base, w_first, w_step, total, q, half, lane, rank, abortp);
     }
   } else if (B_MN) {
     // ------------------------------------------------------------------ fixer
@@ -899,11 +949,11 @@ mbd_status ready(int dev, int* sms) {
 
 template <int KIND, int A_MN, int B_MN>
 cudaError_t launch(const Launch& l, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b32,
-                   const CUtensorMap& out, const CUtensorMap& aux, const Params& p, cudaStream_t stream) {
+                   const CUtensorMap& out, const Params& p, cudaStream_t stream) {
   const dim3 grid(l.grid), block(B_MN ? 352 : 320);
-  if (l.pair) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, grid, block, SMEM_BYTES, stream, 2, a, b, b32, out, aux, p);
-  if (!l.split) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, grid, block, SMEM_BYTES, stream, 1, a, b, b32, out, aux, p);
-  return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, grid, block, SMEM_BYTES, stream, l.split, a, b, b32, out, aux, p);
+  if (l.pair) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, grid, block, SMEM_BYTES, stream, 2, a, b, b32, out, p);
+  if (!l.split) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, grid, block, SMEM_BYTES, stream, 1, a, b, b32, out, p);
+  return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, grid, block, SMEM_BYTES, stream, l.split, a, b, b32, out, p);
 }
 
 // Most units a call can have: a group of c rows is cut into ceil(c / BN) row tiles.
@@ -1018,14 +1068,12 @@ mbd_status run(Call c) {
                    : make_map(&a, c.B, esize, c.d_in, rows, 1, c.ldb, rows * c.ldb, 64) && make_map(&b, c.A, esize, c.d_out, rows, 1, c.lda, rows * c.lda, 64);
     b32 = b;
   }
-  // results (and what the tail operation reads) in boxes of 32 channels, see fill_box
+  // results (and old weights) in boxes of 32 channels, see `epilogue`
   const int osize = t->out_bf16 ? 2 : 4;
-  const uint64_t orows = c.variant == 2 ? c.d_out : rows, odepth = c.variant == 2 ? c.E : 1;
-  CUtensorMap out, aux;
-  ok = ok && make_map(&out, t->out_dev, osize, M, orows, odepth, t->ldo, c.variant == 2 && c.E > 1 ? c.stride : orows * t->ldo, t->out_bf16 ? 32 : 16, 32 * osize, false);
-  aux = out;
-  if (t->op == MBD_TAIL_MASK && t->mask_dev)
-    ok = ok && make_map(&aux, t->mask_dev, osize, M, orows, 1, t->ldmask, orows * t->ldmask, t->out_bf16 ? 32 : 16, 32 * osize, false);
+  const uint64_t orows = c.variant == 2 ? c.d_out : rows;
+  CUtensorMap out;
+  ok = ok && make_map(&out, t->out_dev, osize, M, orows, c.variant == 2 ? c.E : 1, t->ldo, c.variant == 2 && c.E > 1 ? c.stride : orows * t->ldo,
+                      t->out_bf16 ? 32 : 16, 32 * osize, false);
   if (!ok) return MBD_E_CUDA;
 
   Params p{};
@@ -1060,10 +1108,10 @@ mbd_status run(Call c) {
   }
   p.status = word;
   cudaError_t e;
-  if (c.kind == KIND_I8) e = launch<KIND_I8, 0, 0>(l, a, b, b32, out, aux, p, stream);
-  else if (c.variant == 0) e = launch<KIND_BF16, 0, 0>(l, a, b, b32, out, aux, p, stream);
-  else if (c.variant == 1) e = launch<KIND_BF16, 1, 0>(l, a, b, b32, out, aux, p, stream);
-  else e = launch<KIND_BF16, 1, 1>(l, a, b, b32, out, aux, p, stream);
+  if (c.kind == KIND_I8) e = launch<KIND_I8, 0, 0>(l, a, b, b32, out, p, stream);
+  else if (c.variant == 0) e = launch<KIND_BF16, 0, 0>(l, a, b, b32, out, p, stream);
+  else if (c.variant == 1) e = launch<KIND_BF16, 1, 0>(l, a, b, b32, out, p, stream);
+  else e = launch<KIND_BF16, 1, 1>(l, a, b, b32, out, p, stream);
   mbd_status ret = e == cudaSuccess ? MBD_OK : MBD_E_CUDA;
   if (c.status) {                          // enqueue-only: the caller owns and reads the status word
     if (ret != MBD_OK) (void)cudaGetLastError();
