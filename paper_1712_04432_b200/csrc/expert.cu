@@ -19,6 +19,8 @@
 // The split form cuts K over the CTAs of a cluster and joins the pieces through distributed shared memory, for calls
 // with too few tiles to keep the SMs busy.
 // Every wait is bounded; on time-out the kernel records a code and leaves.
+#include <math.h>
+
 #include <atomic>
 
 #include "../../include/mbd.h"
@@ -555,7 +557,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   constexpr int ACC_BUFS = SPLIT ? 1 : 2;
   constexpr int TMEM_COLS = ACC_BUFS * BN;
   constexpr int ELEMS = KIND == KIND_I8 ? 128 : 64;          // elements of a k-block
-  static_assert(TMEM_COLS >= 32 && TMEM_COLS <= 512 && STAGES <= 16 && (BNL == 64 || BNL == 128), "");
+  static_assert(TMEM_COLS >= 32 && TMEM_COLS <= 512 && STAGES <= 16 && (BNL == 64 || BNL == 128 || BNL == 256) &&
+                !(SPLIT && BN * CH * 4 > RING_BYTES), "");
 
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Groups groups;
@@ -601,12 +604,16 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       tmem_alloc<TMEM_COLS>(smem_u32(&tmem_slot));
     }
   }
+  if (warp == 2 && lane < 3) {             // the maps are the launch's own: they may be fetched before the kernel before this one is done
+    const CUtensorMap* tm = lane == 0 ? &tmA : lane == 1 ? &tmB : &tmB32;
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
+  }
   pdl_trigger();
   pdl_wait();                              // the offsets may come from the kernel before this one
   if (warp == 0) find_groups<BN>(p, &groups, lane);
   tc_fence_before();
   __syncthreads();
-  if (PAIR || SPLIT) cluster_sync();       // the other CTAs' barriers exist before anything remote touches them
+  if (PAIR) cluster_sync();                // the other CTA's barriers exist before anything remote touches them (SPLIT meets below)
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   const int total = total_units<B_MN, BN, PAIR>(p, &groups);
@@ -696,10 +703,11 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
           }
         };
         auto by_rows = [&](auto chunked_c) {
-          if (half > BNL - 32) k_blocks(Int<0>{}, chunked_c);
+          if (half > (BNL == 256 ? 128 : BNL - 32)) k_blocks(Int<0>{}, chunked_c);
           else if (BNL <= 64 || half <= 32) k_blocks(Int<1>{}, chunked_c);
           else if (half <= 64) k_blocks(Int<2>{}, chunked_c);
-          else k_blocks(Int<3>{}, chunked_c);
+          else if (BNL <= 128 || half <= 96) k_blocks(Int<3>{}, chunked_c);
+          else k_blocks(Int<4>{}, chunked_c);
         };
         if (B_MN) {
           if (p.chunked_a && p.chunked_b) k_blocks(Int<BNL / 64>{}, Int<3>{});
@@ -919,16 +927,19 @@ bool make_chunk_map(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t 
 constexpr int MAX_DEVICES = 64;
 
 struct Launch {
-  int BN, pair, split;       // split: CTAs that share a unit's K range; 0: the persistent form
+  int BN, pair, split;       // split: CTAs that share a unit's K range; 0: the persistent forms
   int grid;
 };
 
 template <int KIND, int A_MN, int B_MN>
 cudaError_t set_attributes() {
+  constexpr cudaFuncAttribute SIZE = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e;
-  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES)) != cudaSuccess) return e;
-  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES)) != cudaSuccess) return e;
-  return cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, SIZE, SMEM_BYTES)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, SIZE, SMEM_BYTES)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, SIZE, SMEM_BYTES)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 128, 0, 1>, SIZE, SMEM_BYTES)) != cudaSuccess) return e;
+  return cudaFuncSetAttribute(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 0, 1>, SIZE, SMEM_BYTES);
 }
 
 // What a device needs before its first launch, and how many SMs it has.  (The opt-in to large shared memory is per device; two threads
@@ -953,7 +964,9 @@ cudaError_t launch(const Launch& l, const CUtensorMap& a, const CUtensorMap& b, 
   const dim3 grid(l.grid), block(B_MN ? 352 : 320);
   if (l.pair) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 1, 0>, grid, block, SMEM_BYTES, stream, 2, a, b, b32, out, p);
   if (!l.split) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 0>, grid, block, SMEM_BYTES, stream, 1, a, b, b32, out, p);
-  return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, grid, block, SMEM_BYTES, stream, l.split, a, b, b32, out, p);
+  if (l.BN == 64) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 64, 0, 1>, grid, block, SMEM_BYTES, stream, l.split, a, b, b32, out, p);
+  if (l.BN == 128) return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 128, 0, 1>, grid, block, SMEM_BYTES, stream, l.split, a, b, b32, out, p);
+  return launch_pdl(expert_gemm_kernel<KIND, A_MN, B_MN, 256, 0, 1>, grid, block, SMEM_BYTES, stream, l.split, a, b, b32, out, p);
 }
 
 // Most units a call can have: a group of c rows is cut into ceil(c / BN) row tiles.
@@ -964,27 +977,45 @@ int64_t most_units(int variant, int E, int64_t T, int64_t M, int64_t N, int BN, 
   return mt * (E == 1 ? (T + BN - 1) / BN : T / BN + groups);
 }
 
+// The form of a call, by a model in SM clocks: waves of tiles over the SMs (or pairs of them), a tile's k-blocks, what a tile costs
+// beside them and, for the split forms, joining the pieces.  A k-block costs four instructions of at least 100 clocks whatever their
+// number of rows (540 for a pair, measured: halving a pair's rows took 8 % off a tile's time), or filling shared memory at about 70 bytes a
+// clock.  The group sizes are not known here: rows spread evenly over the experts they can touch, a tile and a half each beyond one.
+// Measured with 16 rows of K = 9216 int8 on 4096 channels: 28 us by the pair form, 12.9 us split in 4; 8192 rows: 0.31 ms by the pair
+// form, and 128-row tiles twice that.
 Launch plan(int kind, int variant, int E, int64_t T, int64_t M, int64_t N, int64_t K, bool out_f32, int sms) {
-  Launch l{256, 1, 0, 0};
-  const int64_t rows = variant == 2 ? N : (T + E - 1) / E;       // output rows of a group, on average
   const int64_t per_kb = kind == KIND_I8 ? 128 : 64;
-  const int64_t k = variant == 2 ? (T + E - 1) / E : K;
-  if (rows <= 64) {
-    l.BN = 64;
-    l.pair = 0;
-    const int64_t units = most_units(variant, E, T, M, N, 64, CH);
-    const int64_t kbs = (k + per_kb - 1) / per_kb;
-    int s = 0;
-    for (int c = 2; c <= 8; c *= 2)
-      if (units * c <= sms && kbs / c >= 4) s = c;
-    if (out_f32 && kind == KIND_BF16 && s && (variant == 2 ? T : K) / s > 64 * SEG_BLOCKS) s = 0;
-    l.split = s;
-  }
-  const int64_t units = most_units(variant, E, T, M, N, l.BN, l.pair ? 2 * CH : CH);
-  if (l.split) l.grid = static_cast<int>(units * l.split);
-  else if (l.pair) l.grid = static_cast<int>(2 * (units < sms / 2 ? units : sms / 2));
-  else l.grid = static_cast<int>(units < sms ? units : sms);
-  return l;
+  const double groups = variant == 2 ? E : static_cast<double>(E < T ? E : T);
+  const double rows = variant == 2 ? static_cast<double>(N) : static_cast<double>(T) / groups;      // output rows of a group
+  const double k = variant == 2 ? static_cast<double>(T) / E : static_cast<double>(K);
+  const double kbs = k / per_kb > 1.0 ? k / per_kb : 1.0;
+  const double longest = static_cast<double>(variant == 2 ? T : K);                                // of a sum
+  Launch best{256, 1, 0, 0};
+  double least = 1e30;
+  const auto consider = [&](int BN, int pair, int split) {
+    const double tiles = rows <= BN ? groups : variant == 2 ? groups * ((N + BN - 1) / BN) : groups * (rows / BN + (E > 1 ? 0.5 : 0.0));
+    const double units = ceil(tiles) * static_cast<double>((M + (pair ? 2 : 1) * CH - 1) / ((pair ? 2 : 1) * CH));
+    const double nt = rows < BN ? rows : BN;
+    const double mma = pair ? 540.0 : 4.0 * (nt / 2 > 100.0 ? nt / 2 : 100.0), fill = (CH + (pair ? nt / 2 : nt)) * 128.0 / 70.0;
+    const int pieces = split > 1 ? split : 1;
+    const double waves = ceil(units * pieces / (pair ? sms / 2 : sms));
+    const double t = waves * (kbs / pieces * (mma > fill ? mma : fill) + 3000.0) + (pieces > 1 ? 4000.0 : 0.0);
+    if (t < least) { least = t; best = Launch{BN, pair, split, 0}; }
+  };
+  consider(256, 1, 0);
+  consider(64, 0, 0);
+  for (int BN = 64; BN <= 256; BN *= 2)
+    for (int s = 2; s <= 8; s *= 2) {
+      if (kbs / s < 4.0) continue;
+      if (out_f32 && kind == KIND_BF16 && longest / s > 64.0 * SEG_BLOCKS) continue;               // (a piece is one segment)
+      if (most_units(variant, E, T, M, N, BN, CH) * s > (1 << 30)) continue;
+      consider(BN, 0, s);
+    }
+  const int64_t units = most_units(variant, E, T, M, N, best.BN, best.pair ? 2 * CH : CH);
+  if (best.split) best.grid = static_cast<int>(units * best.split);
+  else if (best.pair) best.grid = static_cast<int>(2 * (units < sms / 2 ? units : sms / 2));
+  else best.grid = static_cast<int>(units < sms ? units : sms);
+  return best;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -113,6 +113,9 @@ CASES = [
     ([17, 129], 0, 0, 37, 41, None),                        # odd sizes in padded rows
     ([1, 255, 256, 257, 1], 2, 2, 1001, 131, None),
     ([1000], 0, 24, 16, 8, 0),
+    ([120, 70], 0, 3, 4096, 256, 0),                        # long K and few tiles of 65 - 256 rows: the other split forms
+    ([200], 5, 0, 256, 4104, 0),
+    ([2000, 1100], 0, 0, 136, 72, 0),                       # variant 2: long groups, few tiles
 ]
 
 

@@ -140,7 +140,7 @@ def _close(got, ref, dtype, mag):
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 8, 16), (16, 128, 4096), (3, 1000, 200), (64, 72, 1040), (65, 264, 128), (300, 520, 272),
-                                   (513, 131, 1001), (2, 4096, 9216), (1000, 24, 48)])
+                                   (513, 131, 1001), (2, 4096, 9216), (1000, 24, 48), (128, 520, 9216), (250, 264, 4112), (700, 136, 8208)])
 def test_dense(M, N, K, dtype):
     import torch
     gen = torch.Generator(device="cuda")
