@@ -116,7 +116,11 @@ enum {
   MBD_T_PARTIALS = 5, /* fp32 partial-sum workspace as left by the LAST reduction executed   */
   MBD_T_MASTER = 6,   /* fp32 master weights, weight shape (get only; after mbd_enable_master_weights) */
   MBD_T_VELOCITY = 7, /* momentum velocity of W_i, float, weight shape (get only; after mbd_enable_momentum) */
-  MBD_T_VELOCITY_BIAS = 8 /* momentum velocity of b_i, float [d_i] (fully connected layers with a bias)    */
+  MBD_T_VELOCITY_BIAS = 8, /* momentum velocity of b_i, float [d_i] (fully connected layers with a bias)   */
+  MBD_T_ADAM_M = 9,   /* AdamW's moments of W_i, float, weight shape, and of b_i, float [d_i] (get only;      */
+  MBD_T_ADAM_V = 10,  /* after mbd_enable_adamw with moments in 32 bits)                                      */
+  MBD_T_ADAM_M_BIAS = 11,
+  MBD_T_ADAM_V_BIAS = 12
 };
 
 /* Section 2.3 / 2.4.  Builds the plan for an L-layer network on batch B over a
@@ -193,6 +197,15 @@ MBD_API mbd_status mbd_enable_master_weights(mbd_net* net);
  * master weights are on, the bf16 weights being its rounding.  mbd_sgd_step does the same from the stored
  * gradients.  Calling it again resets the velocities and sets a new mu.  MBD_E_INVALID for mu outside [0, 1). */
 MBD_API mbd_status mbd_enable_momentum(mbd_net* net, float mu);
+
+/* Optional, fully connected networks: AdamW in place of Eq. 1 (see "AdamW over many tensors" below for the formulas), on the
+ * gradients dW_i / B and db_i / B with eta as the learning rate: mbd_backward with fused_eta > 0 materialises every dW_i and one launch
+ * updates all layers at the end, mbd_sgd_step does the same from the stored gradients, and mbd_train_step captures it (the step count
+ * lives on the device).  weight_decay applies to the W_i, not to biases.  state_bits 32 or 8: how the moments are held.  The moments are
+ * zero and the step count 0 when this call returns; calling it again resets them.  Of momentum and AdamW the one enabled last is in
+ * force.  With master weights the masters are what is updated (in whichever order the two are enabled).  MBD_E_INVALID for rates outside
+ * [0, 1), eps outside [1e-30, 1) or a negative decay, MBD_E_UNSUPPORTED for networks with convolutions and other state_bits. */
+MBD_API mbd_status mbd_enable_adamw(mbd_net* net, double beta1, double beta2, double eps, float weight_decay, int state_bits);
 
 /* Copy weights (network dtype) and bias (float, may be NULL) device -> library / back. */
 MBD_API mbd_status mbd_set_weights(mbd_net* net, int layer, const void* W_dev, const float* bias_dev);

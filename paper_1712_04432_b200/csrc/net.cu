@@ -32,6 +32,8 @@ struct Layer {
   float* W32 = nullptr;  // fp32 master weights (optional)
   float* V = nullptr;    // momentum: velocity of W (optional), fp32
   float* Vb = nullptr;   // momentum: velocity of the bias
+  void *Am = nullptr, *Av = nullptr, *Abm = nullptr, *Abv = nullptr;             // AdamW: moments of W and of the bias (optional)
+  float *Ams = nullptr, *Avs = nullptr, *Abms = nullptr, *Abvs = nullptr;       // AdamW with moments in 8 bits: their scales
   float* db = nullptr;
   void* act = nullptr;   // stored forward output [B, d_out]; float logits for the last FC layer
   void* dY = nullptr;    // [B, d_out] activation dtype
@@ -55,6 +57,10 @@ struct mbd_net {
   bool master = false;              // fp32 master weights: the update leaves the contraction's epilogue
   bool momentum = false;            // heavy-ball momentum: the update is a kernel of its own after the gradient
   float mu = 0.f;
+  mbd_adamw* adamw = nullptr;       // AdamW: one launch over all tensors after the gradients
+  double adam_b1 = 0, adam_b2 = 0, adam_eps = 0;
+  float adam_decay = 0.f;
+  int adam_bits = 32;
   std::vector<Layer> layers;
   float* partials = nullptr;
   size_t partial_elems = 0;
@@ -250,10 +256,52 @@ mbd_status map_input(mbd_net* n) {
   return MBD_OK;
 }
 
+void free_moments(Layer& l) {
+  for (void* p : {l.Am, l.Av, l.Abm, l.Abv}) cudaFree(p);
+  for (float* p : {l.Ams, l.Avs, l.Abms, l.Abvs}) cudaFree(p);
+  l.Am = l.Av = l.Abm = l.Abv = nullptr;
+  l.Ams = l.Avs = l.Abms = l.Abvs = nullptr;
+}
+
+// The network's tensors as one AdamW list: every W_i (its fp32 master if there is one) and, without decay, every bias.
+mbd_status make_adamw_list(mbd_net* n, int64_t steps) {
+  std::vector<mbd_adamw_tensor> list;
+  for (Layer& l : n->layers) {
+    mbd_adamw_tensor t{};
+    t.param_dev = l.W; t.master_dev = l.W32; t.grad_dev = l.dW; t.m_dev = l.Am; t.v_dev = l.Av; t.m_scale_dev = l.Ams; t.v_scale_dev = l.Avs;
+    t.n = l.nW; t.weight_decay = n->adam_decay; t.param_bf16 = n->dtype == MBD_BF16;
+    list.push_back(t);
+    if (!l.bias) continue;
+    t = mbd_adamw_tensor{};
+    t.param_dev = l.bias; t.grad_dev = l.db; t.m_dev = l.Abm; t.v_dev = l.Abv; t.m_scale_dev = l.Abms; t.v_scale_dev = l.Abvs; t.n = l.d_out;
+    list.push_back(t);
+  }
+  mbd_adamw* fresh = nullptr;
+  const mbd_status s = mbd_adamw_create(list.data(), static_cast<int>(list.size()), n->adam_bits, n->adam_b1, n->adam_b2, n->adam_eps, steps, &fresh);
+  if (s != MBD_OK) return s;
+  if (n->adamw) mbd_adamw_destroy(n->adamw);
+  n->adamw = fresh;
+  return MBD_OK;
+}
+
+// The AdamW step over all layers from the materialised gradients, on the network's stream.
+mbd_status adamw_update(mbd_net* n, float eta) {
+  double bytes = 0;
+  const double moments = n->adam_bits == 32 ? 16.0 : 4.0 + 16.0 / 256.0;
+  for (const Layer& l : n->layers)
+    bytes += l.nW * (moments + 4.0 + (l.W32 ? 10.0 : 2.0 * (n->dtype == MBD_BF16 ? 2.0 : 4.0))) + (l.bias ? l.d_out * (moments + 12.0) : 0.0);
+  n->prof.begin(MBD_K_SGD, bytes);
+  const mbd_status s = mbd_adamw_step(n->adamw, eta, 1.0 / static_cast<double>(n->B), n->stream);
+  n->prof.end();
+  return s;
+}
+
 void free_net(mbd_net* n) {
   if (!n) return;
+  if (n->adamw) mbd_adamw_destroy(n->adamw);
   for (Layer& l : n->layers) {
     cudaFree(l.W); cudaFree(l.bias); cudaFree(l.dW); cudaFree(l.db); cudaFree(l.act); cudaFree(l.dY); cudaFree(l.W32); cudaFree(l.V); cudaFree(l.Vb);
+    free_moments(l);
   }
   cudaFree(n->partials); cudaFree(n->colsum_scratch); cudaFree(n->colsum_scratch_aux); cudaFree(n->per_sample); cudaFree(n->loss_dev);
   cudaFree(n->status); cudaFree(n->X_stage); cudaFree(n->labels_stage); cudaFree(n->X_fc); cudaFree(n->dX_fc);
@@ -519,6 +567,12 @@ extern "C" mbd_status mbd_enable_master_weights(mbd_net* n) {
     CK(widen_bf16_launch(l.W, l.W32, l.nW, n->num_sms, n->stream));
   }
   n->master = true;
+  if (n->adamw) {                    // the list names the masters from now on; moments and step count go on
+    int64_t steps = 0;
+    mbd_status s = mbd_adamw_get_steps(n->adamw, &steps);
+    if (s == MBD_OK) s = make_adamw_list(n, steps);
+    if (s != MBD_OK) return s;
+  }
   if (n->graph_exec) { cudaGraphExecDestroy(n->graph_exec); n->graph_exec = nullptr; }   // the step's launches change
   return MBD_OK;
 }
@@ -540,6 +594,48 @@ extern "C" mbd_status mbd_enable_momentum(mbd_net* n, float mu) {
   }
   n->momentum = true;
   n->mu = mu;
+  if (n->adamw) { mbd_adamw_destroy(n->adamw); n->adamw = nullptr; }                     // one method at a time: the one enabled last
+  if (n->graph_exec) { cudaGraphExecDestroy(n->graph_exec); n->graph_exec = nullptr; }   // the step's launches change
+  return MBD_OK;
+}
+
+extern "C" mbd_status mbd_enable_adamw(mbd_net* n, double beta1, double beta2, double eps, float weight_decay, int state_bits) {
+  if (!n || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 1e-30 && eps < 1.0) ||
+      !(weight_decay >= 0.f && weight_decay < 1e30f)) return MBD_E_INVALID;
+  if (n->conv || (state_bits != 32 && state_bits != 8)) return MBD_E_UNSUPPORTED;
+  const bool again = n->adamw && n->adam_bits == state_bits;
+  if (!again) {
+    CK(cudaStreamSynchronize(n->stream));                    // a step under way may still use the moments that go
+    if (n->adamw) { mbd_adamw_destroy(n->adamw); n->adamw = nullptr; }
+    for (Layer& l : n->layers) free_moments(l);
+  }
+  const auto zeros = [&](void** p, size_t bytes) -> mbd_status {
+    if (!*p) {
+      const mbd_status s = dev_alloc(p, bytes);
+      if (s != MBD_OK) return s;
+    }
+    CK(cudaMemsetAsync(*p, 0, bytes, n->stream));
+    return MBD_OK;
+  };
+  const size_t each = state_bits == 32 ? 4 : 1;
+  for (Layer& l : n->layers) {
+    mbd_status s = zeros(&l.Am, l.nW * each);
+    if (s == MBD_OK) s = zeros(&l.Av, l.nW * each);
+    if (s == MBD_OK && l.bias) s = zeros(&l.Abm, l.d_out * each);
+    if (s == MBD_OK && l.bias) s = zeros(&l.Abv, l.d_out * each);
+    if (state_bits == 8) {
+      const size_t w = (l.nW + 255) / 256 * sizeof(float), b = (l.d_out + 255) / 256 * sizeof(float);
+      if (s == MBD_OK) s = zeros(reinterpret_cast<void**>(&l.Ams), w);
+      if (s == MBD_OK) s = zeros(reinterpret_cast<void**>(&l.Avs), w);
+      if (s == MBD_OK && l.bias) s = zeros(reinterpret_cast<void**>(&l.Abms), b);
+      if (s == MBD_OK && l.bias) s = zeros(reinterpret_cast<void**>(&l.Abvs), b);
+    }
+    if (s != MBD_OK) return s;
+  }
+  n->adam_b1 = beta1; n->adam_b2 = beta2; n->adam_eps = eps; n->adam_decay = weight_decay; n->adam_bits = state_bits;
+  const mbd_status s = make_adamw_list(n, 0);
+  if (s != MBD_OK) return s;
+  n->momentum = false;
   if (n->graph_exec) { cudaGraphExecDestroy(n->graph_exec); n->graph_exec = nullptr; }   // the step's launches change
   return MBD_OK;
 }
@@ -632,7 +728,7 @@ extern "C" mbd_status mbd_backward(mbd_net* n, float fused_eta) {
         forked = true;
       }
       n->prof.begin(MBD_K_COLSUM, static_cast<double>(n->B) * l.d_out * (bf ? 2.0 : 4.0), cs);
-      const bool fused_b = fused && !n->momentum;          // momentum: db first, then the update kernel
+      const bool fused_b = fused && !n->momentum && !n->adamw;          // momentum, AdamW: db first, then the update kernel
       CK(colsum_launch(l.dY, bf, n->B, l.d_out, cs == n->aux ? n->colsum_scratch_aux : n->colsum_scratch, colsum_row_splits(n->B, l.d_out, n->num_sms), fused_b ? nullptr : l.db,
                        fused_b ? l.bias : nullptr, scale, cs));
       n->prof.end();
@@ -651,9 +747,9 @@ extern "C" mbd_status mbd_backward(mbd_net* n, float fused_eta) {
     // With master weights: a split product updates the fp32 master in the tail of its reduction (which streams
     // the sum through registers anyway); an unsplit one materialises the gradient and a streaming kernel applies
     // Eq. 1 to the master (measured equal to doing it in the product's epilogue, whose loads would be exposed).
-    const bool master_tail = fused && n->master && !n->momentum && bf && l.bwd_weight.k_splits > 1;
-    const bool master_kernel = fused && (n->master || n->momentum) && !master_tail;     // momentum: always a kernel of its own
-    const Epi e = (fused && !master_kernel) ? epi_sgd(l.W, l.d_in, bf, scale, master_tail ? l.W32 : nullptr)
+    const bool master_tail = fused && n->master && !n->momentum && !n->adamw && bf && l.bwd_weight.k_splits > 1;
+    const bool master_kernel = fused && (n->master || n->momentum) && !n->adamw && !master_tail;     // momentum: always a kernel of its own
+    const Epi e = (fused && !master_kernel && !n->adamw) ? epi_sgd(l.W, l.d_in, bf, scale, master_tail ? l.W32 : nullptr)
                                             : epi_act(l.dW, l.d_in, 0, nullptr, 0);
     cudaStream_t ws = nullptr;
     if (n->overlap_dw) {
@@ -686,6 +782,10 @@ extern "C" mbd_status mbd_backward(mbd_net* n, float fused_eta) {
     CK(cudaEventRecord(n->ev_join, n->aux));
     CK(cudaStreamWaitEvent(n->stream, n->ev_join, 0));
   }
+  if (fused && n->adamw) {           // every gradient is there: one launch for all layers
+    const mbd_status s = adamw_update(n, fused_eta);
+    if (s != MBD_OK) return s;
+  }
   if (n->mixed) {
     // the gradient of the first fully connected layer's input goes back into strips and down the convolutions
     mbd_status s = conv_top_grad_from_nchw(n->conv, n->dX_fc);
@@ -708,6 +808,11 @@ extern "C" mbd_status mbd_sgd_step(mbd_net* n, float eta) {
   if (n->mixed) {
     mbd_status s = conv_sgd_step(n->conv, eta);
     if (s != MBD_OK) return s;
+  }
+  if (n->adamw) {
+    const mbd_status s = adamw_update(n, eta);
+    if (s == MBD_OK) n->state = ST_IDLE;
+    return s;
   }
   for (int i = 0; i < n->L; ++i) {
     Layer& l = n->layers[i];
@@ -880,6 +985,10 @@ extern "C" mbd_status mbd_get_tensor(mbd_net* n, int which, int layer, void* dst
       case MBD_T_MASTER: src = l.W32; size = l.nW * sizeof(float); break;
       case MBD_T_VELOCITY: src = l.V; size = l.nW * sizeof(float); break;
       case MBD_T_VELOCITY_BIAS: src = l.Vb; size = l.d_out * sizeof(float); break;
+      case MBD_T_ADAM_M: src = n->adam_bits == 32 ? l.Am : nullptr; size = l.nW * sizeof(float); break;
+      case MBD_T_ADAM_V: src = n->adam_bits == 32 ? l.Av : nullptr; size = l.nW * sizeof(float); break;
+      case MBD_T_ADAM_M_BIAS: src = n->adam_bits == 32 ? l.Abm : nullptr; size = l.d_out * sizeof(float); break;
+      case MBD_T_ADAM_V_BIAS: src = n->adam_bits == 32 ? l.Abv : nullptr; size = l.d_out * sizeof(float); break;
       case MBD_T_DB: src = l.db; size = l.d_out * sizeof(float); break;
       default: return MBD_E_INVALID;
     }

@@ -18,7 +18,7 @@ FC, CONV3X3 = 0, 1
 SPLIT_MODEL, SPLIT_DOMAIN, SPLIT_BATCH = 0, 1, 2
 F32, BF16 = 0, 1
 LOSS_SOFTMAX_CE, LOSS_HALF_SSQ, LOSS_NONE = 0, 1, 2
-T_ACT, T_DY, T_DW, T_DB, T_LOSS, T_PARTIALS, T_MASTER, T_VELOCITY, T_VELOCITY_BIAS = range(9)
+T_ACT, T_DY, T_DW, T_DB, T_LOSS, T_PARTIALS, T_MASTER, T_VELOCITY, T_VELOCITY_BIAS, T_ADAM_M, T_ADAM_V, T_ADAM_M_BIAS, T_ADAM_V_BIAS = range(13)
 ROWS_ALL, ROWS_INTERIOR, ROWS_BOUNDARY = range(3)
 
 KERNEL_CLASSES = ["gemm_fwd", "gemm_bwd_data", "gemm_bwd_weight", "reduce_partials", "softmax_xent", "colsum",
@@ -33,7 +33,7 @@ EXPORTS = ["mbd_net_create", "mbd_net_destroy", "mbd_set_weights", "mbd_get_weig
            "mbd_conv_stage_input", "mbd_conv_forward_layer", "mbd_conv_backward_layer", "mbd_conv_outer_rows",
            "mbd_get_plan", "mbd_plan_product", "mbd_conv_forward_layer_rows", "mbd_conv_backward_layer_rows",
            "mbd_expert_gemm_bf16", "mbd_quantize_rows", "mbd_gemm_i8", "mbd_expert_gemm_i8",
-           "mbd_adamw_create", "mbd_adamw_destroy", "mbd_adamw_step", "mbd_adamw_set_steps", "mbd_adamw_get_steps"]
+           "mbd_enable_adamw", "mbd_adamw_create", "mbd_adamw_destroy", "mbd_adamw_step", "mbd_adamw_set_steps", "mbd_adamw_get_steps"]
 
 
 class MbdError(RuntimeError):
@@ -159,6 +159,7 @@ def lib():
         L.mbd_expert_gemm_i8.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, vp, i64, i64, vp, C.POINTER(Tail), vp, vp]
         L.mbd_adamw_create.argtypes = [C.POINTER(AdamWTensor), i32, i32, f64, f64, f64, i64, C.POINTER(vp)]
         L.mbd_adamw_destroy.argtypes = [vp]
+        L.mbd_enable_adamw.argtypes = [vp, f64, f64, f64, f32, i32]
         L.mbd_adamw_step.argtypes = [vp, f64, f64, vp]
         L.mbd_adamw_set_steps.argtypes = [vp, i64]
         L.mbd_adamw_get_steps.argtypes = [vp, C.POINTER(i64)]
@@ -369,6 +370,11 @@ class Net:
         """Heavy-ball momentum from now on, velocities zero (see include/mbd.h)."""
         _check(lib().mbd_enable_momentum(self._h, float(mu)), "mbd_enable_momentum")
 
+    def enable_adamw(self, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, state_bits: int = 32):
+        """AdamW from now on, moments zero (see include/mbd.h); eta is its learning rate.  Fully connected networks."""
+        _check(lib().mbd_enable_adamw(self._h, float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(state_bits)),
+               "mbd_enable_adamw")
+
     def backward(self, fused_eta: float = 0.0):
         _check(lib().mbd_backward(self._h, float(fused_eta)), "mbd_backward")
 
@@ -411,9 +417,9 @@ class Net:
                 (t.float32 if (last and not conv) else self.act_dtype)
         elif which == T_DY:
             shape, dt = ((self.B, l.C_out, l.H // max(1, l.stride), l.W // max(1, l.stride)) if conv else (self.B, l.d_out)), self.act_dtype
-        elif which in (T_DW, T_MASTER, T_VELOCITY):
+        elif which in (T_DW, T_MASTER, T_VELOCITY, T_ADAM_M, T_ADAM_V):
             shape, dt = self._wshape(layer), t.float32
-        elif which in (T_DB, T_VELOCITY_BIAS):
+        elif which in (T_DB, T_VELOCITY_BIAS, T_ADAM_M_BIAS, T_ADAM_V_BIAS):
             shape, dt = (l.d_out,), t.float32
         elif which == T_LOSS:
             shape, dt = (self.B,), t.float32
