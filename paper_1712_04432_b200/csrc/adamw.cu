@@ -234,6 +234,7 @@ __device__ __forceinline__ bool encode(const f32x2* x, const f32x2* approx, floa
 struct Rates {
   f32x2 grad, b1, c1, b2, c2, root, eps, step;      // each twice
   float lr;
+  bool exact_root;
 };
 
 // What a lane holds of a warp's block of 256: elements 4 l .. 4 l + 3 of either half.  There is a copy of the loop for each
@@ -359,6 +360,16 @@ __device__ __forceinline__ void update(const Raw<BITS>& raw, float& ms, float& v
     v[i] = add2(mul2(v[i], r.b2), mul2(mul2(g[i], g[i]), r.c2));
     const float2 vf = floats(v[i]);
     root[i] = pair(approx_root(vf.x), approx_root(vf.y));
+  }
+  if (r.exact_root) {                  // (approximate roots below 1e-19 are zero: that is seen next to a very small eps only)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 vf = floats(v[i]);
+      root[i] = pair(__fsqrt_rn(vf.x), __fsqrt_rn(vf.y));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
     const float2 d = floats(fma2(root[i], r.root, r.eps));
     const f32x2 move = mul2(m[i], pair(approx_reciprocal(d.x), approx_reciprocal(d.y)));
     x[i] = fma2(move, r.step, mul2(x[i], keep2));
@@ -462,7 +473,7 @@ adamw_kernel(const Tensor* __restrict__ tensors, const int* __restrict__ first, 
     const long long t = clock->t;
     const auto both = [](double x) { return pair(static_cast<float>(x), static_cast<float>(x)); };
     rates = Rates{both(grad_scale), both(b1), both(1.0 - b1), both(b2), both(1.0 - b2), both(1.0 / sqrt(1.0 - p2)), both(eps),
-                  both(-lr / (1.0 - p1)), static_cast<float>(lr)};
+                  both(-lr / (1.0 - p1)), static_cast<float>(lr), eps < 1e-12f};
     // the block that comes last has read the clock after every other one, and moves it on
     __threadfence();
     if (atomicAdd(&clock->seen, 1u) == gridDim.x - 1) {
@@ -607,7 +618,7 @@ extern "C" mbd_status mbd_adamw_create(const mbd_adamw_tensor* tensors_host, int
     }
     *out = h;
     return MBD_OK;
-  } catch (const std::bad_alloc&) {
+  } catch (...) {                      // out of host memory
     return MBD_E_ALLOC;
   }
 }

@@ -905,7 +905,7 @@ EncodeTiledFn encode_fn() {
 bool make_map(CUtensorMap* tm, const void* base, int esize, uint64_t inner, uint64_t rows, uint64_t depth, uint64_t ld, uint64_t plane,
               uint32_t box_rows, uint32_t box_bytes = 128, bool swizzle = true) {
   const cuuint64_t dims[3] = {inner, rows, depth};
-  const cuuint64_t strides[2] = {ld * esize, plane * esize};
+  const cuuint64_t strides[2] = {ld * esize, (depth > 1 ? plane : ld) * esize};         // (one plane: its stride means nothing, but has a limit)
   const cuuint32_t box[3] = {box_bytes / esize, box_rows, 1};
   const cuuint32_t estr[3] = {1, 1, 1};
   return encode_fn()(tm, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : esize == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims,
@@ -917,7 +917,7 @@ bool make_map(CUtensorMap* tm, const void* base, int esize, uint64_t inner, uint
 bool make_chunk_map(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows, uint64_t depth, uint64_t ld, uint64_t plane,
                     uint32_t box_rows, uint32_t chunks) {
   const cuuint64_t dims[4] = {64, rows, inner / 64, depth};
-  const cuuint64_t strides[3] = {ld * 2, 128, plane * 2};
+  const cuuint64_t strides[3] = {ld * 2, 128, (depth > 1 ? plane : ld) * 2};
   const cuuint32_t box[4] = {64, box_rows, chunks, 1};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
   return encode_fn()(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,

@@ -264,7 +264,7 @@ void free_moments(Layer& l) {
 }
 
 // The network's tensors as one AdamW list: every W_i (its fp32 master if there is one) and, without decay, every bias.
-mbd_status make_adamw_list(mbd_net* n, int64_t steps) {
+mbd_status make_adamw_list(mbd_net* n, int64_t steps) try {
   std::vector<mbd_adamw_tensor> list;
   for (Layer& l : n->layers) {
     mbd_adamw_tensor t{};
@@ -282,6 +282,8 @@ mbd_status make_adamw_list(mbd_net* n, int64_t steps) {
   if (n->adamw) mbd_adamw_destroy(n->adamw);
   n->adamw = fresh;
   return MBD_OK;
+} catch (...) {
+  return MBD_E_ALLOC;
 }
 
 // The AdamW step over all layers from the materialised gradients, on the network's stream.

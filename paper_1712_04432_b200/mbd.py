@@ -564,6 +564,13 @@ def _at_or_none(t, dev: int):
     return None if t is None else _at(t, dev)
 
 
+def _word(status, dev: int):
+    """Address of a caller's status word, or None."""
+    import torch
+    assert status is None or status.dtype == torch.int32
+    return _at_or_none(status, dev)
+
+
 def _ld(t, shape, stride) -> int:
     """Elements between rows.  A tensor of one row (or none) has no meaningful stride: the row rounded up to what the library asks for."""
     assert stride[-1] == 1 or shape[-1] == 1
@@ -605,7 +612,7 @@ def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bo
     dev, stream = _device()
     sa, sb, so = A.shape, B.shape, offsets.shape
     assert A.dtype == torch.bfloat16 and B.dtype == torch.bfloat16 and offsets.dtype == torch.int32
-    assert len(sa) == 2 and len(so) == 1 and so[0] >= 2 and (so[0] == 2 or offsets.stride(0) == 1)
+    assert len(sa) == 2 and len(so) == 1 and so[0] >= 2 and offsets.stride(0) == 1
     E, T = so[0] - 1, sa[0]
     if variant == 2:
         assert len(sb) == 2 and sb[0] == T
@@ -618,7 +625,7 @@ def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bo
         shape, stacked = (T, d_in if variant else d_out), B
     t = _group_tail(op, out, shape, dev, relu, bias, (E, d_out), mask, scale)
     _check(lib().mbd_expert_gemm_bf16(variant, E, _at(offsets, dev), T, d_out, d_in, _at(A, dev), _ld(A, sa, A.stride()), _at(B, dev),
-                                      _ld(B, sb, B.stride()), stacked.stride(0), C.byref(t), _at_or_none(status, dev), stream),
+                                      _ld(B, sb, B.stride()), stacked.stride(0), C.byref(t), _word(status, dev), stream),
            "mbd_expert_gemm_bf16")
     return out
 
@@ -666,7 +673,7 @@ def gemm_i8(A, a_scale, B, b_scale, out, relu: bool = False, bias=None, status=N
     sa, sb, lda, ldb, t = _i8(A, a_scale, B, b_scale, out, relu, bias, dev)
     assert len(sb) == 2
     _check(lib().mbd_gemm_i8(sa[0], sb[0], sa[1], _at(A, dev), lda, _at(a_scale, dev), _at(B, dev), ldb, _at(b_scale, dev), C.byref(t),
-                             _at_or_none(status, dev), stream), "mbd_gemm_i8")
+                             _word(status, dev), stream), "mbd_gemm_i8")
     return out
 
 
@@ -678,7 +685,7 @@ def expert_gemm_i8(A, a_scale, B, b_scale, offsets, out, relu: bool = False, bia
     sa, sb, lda, ldb, t = _i8(A, a_scale, B, b_scale, out, relu, bias, dev)
     assert len(sb) == 3 and offsets.dtype == torch.int32 and offsets.is_contiguous() and offsets.shape == (sb[0] + 1,)
     _check(lib().mbd_expert_gemm_i8(sb[0], _at(offsets, dev), sa[0], sb[1], sb[2], _at(A, dev), lda, _at(a_scale, dev), _at(B, dev), ldb,
-                                    B.stride(0), _at(b_scale, dev), C.byref(t), _at_or_none(status, dev), stream), "mbd_expert_gemm_i8")
+                                    B.stride(0), _at(b_scale, dev), C.byref(t), _word(status, dev), stream), "mbd_expert_gemm_i8")
     return out
 
 

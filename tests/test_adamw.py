@@ -289,3 +289,18 @@ def test_many_tensors_and_bad_rates():
         assert e.value.status == mbd.E_INVALID
     assert opt.steps_done == 1
     opt.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_very_small_eps_and_very_small_gradients(bits):
+    # eps beside roots that are themselves tiny: v is a denormal number, its root an ordinary one.  Four roundings in v near 1e-40 (its step
+    # there is 1.4e-45: 7e-6 relative at 1e-40), halved by the root
+    import torch
+    g = torch.tensor([1e-18, -3e-19, 2e-18, 5e-19] * 64, device="cuda")
+    p = torch.zeros(256, device="cuda")
+    opt = mbd.AdamW([p], [g], eps=1e-20, state_bits=bits)
+    opt.step(0.01)
+    want, _, _ = _step(np.zeros(256), g.double().cpu().numpy(), np.zeros(256), np.zeros(256), 1, 0.01, 0.0, eps=1e-20)
+    _near(p.double().cpu().numpy(), want, 1e-4)
+    opt.close()

@@ -383,3 +383,21 @@ def test_gradients_against_differences():
         up[e, n, k] += 1
         down[e, n, k] -= 1
         assert (J(X, up) - J(X, down)) / 2 == float(dW[e, n, k])
+
+
+@pytest.mark.gpu
+def test_the_binding_refuses_what_it_would_misread():
+    import torch
+    X, W, out = torch.zeros(8, 16, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 24, 16, dtype=torch.bfloat16, device="cuda"), torch.zeros(8, 24, device="cuda")
+    ok = torch.tensor([0, 3, 8], dtype=torch.int32, device="cuda")
+    call = lambda **k: mbd.expert_gemm(**{**dict(variant=0, A=X, B=W, offsets=ok, out=out), **k})  # noqa: E731
+    call()
+    for bad in (dict(offsets=ok.long()), dict(offsets=ok.repeat_interleave(2)[::2]), dict(offsets=ok[:2]), dict(offsets=ok.cpu()), dict(variant=3),
+                dict(A=X.float()), dict(A=X[:, :8]), dict(A=X.t()), dict(B=W.transpose(1, 2)), dict(B=W[0]), dict(out=out[:4]), dict(out=out.half()),
+                dict(out=torch.zeros(24, 8, device="cuda").t()), dict(bias=torch.zeros(24, device="cuda")), dict(bias=torch.zeros(2, 24, device="cuda").half()),
+                dict(status=torch.zeros(1, device="cuda")), dict(op=mbd.TAIL_MASK, mask=torch.zeros(8, 24, dtype=torch.bfloat16, device="cuda"))):
+        with pytest.raises(AssertionError):
+            call(**bad)
+    with pytest.raises(mbd.MbdError) as e:
+        call(A=torch.zeros(8, 20, dtype=torch.bfloat16, device="cuda")[:, :16])          # rows 40 bytes apart
+    assert e.value.status == mbd.E_UNSUPPORTED
