@@ -232,7 +232,7 @@ __device__ __forceinline__ bool encode(const f32x2* x, const f32x2* approx, floa
 
 // ------------------------------------------------------------------------------------------------ the step
 struct Rates {
-  f32x2 grad, b1, c1, b2, c2, root, eps, step;      // each twice
+  f32x2 grad, b1, c1, b2, c2, root, eps, step, one; // each twice
   float lr;
   bool exact_root;
 };
@@ -346,8 +346,10 @@ __device__ __forceinline__ void update(const Raw<BITS>& raw, float& ms, float& v
     of_codes(raw.v[0].x, v); of_codes(raw.v[0].y, v + 2);
   }
   const f32x2 ms2 = pair(ms, ms), vs2 = pair(vs, vs), keep2 = pair(keep, keep);
-  // the moments: every product and sum rounded by itself (no fused multiply-add), so that they are the formula's in plain float
-  // arithmetic, bit for bit.  The step taken from them is good to a few units in its own last place.
+  // the moments: every product and sum rounded by itself, so that they are the formula's in plain float arithmetic, bit for bit, and
+  // with them the 8-bit codes (one that falls on the other side of a middle is a sixteenth off).  The compiler joins a packed product and
+  // a packed sum to a fused one; a sum as one * product + product, one known at run time only, it leaves alone.  The step taken from
+  // the moments is good to a few units in its own last place.
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     g[i] = mul2(g[i], r.grad);
@@ -356,8 +358,8 @@ __device__ __forceinline__ void update(const Raw<BITS>& raw, float& ms, float& v
       v[i] = mul2(v[i], vs2);
       v[i] = mul2(v[i], v[i]);
     }
-    m[i] = add2(mul2(m[i], r.b1), mul2(g[i], r.c1));
-    v[i] = add2(mul2(v[i], r.b2), mul2(mul2(g[i], g[i]), r.c2));
+    m[i] = fma2(mul2(m[i], r.b1), r.one, mul2(g[i], r.c1));
+    v[i] = fma2(mul2(v[i], r.b2), r.one, mul2(mul2(g[i], g[i]), r.c2));
     const float2 vf = floats(v[i]);
     root[i] = pair(approx_root(vf.x), approx_root(vf.y));
   }
@@ -465,7 +467,7 @@ __device__ __forceinline__ uint32_t share(const Tensor& w, uint32_t c0, uint32_t
 template <int BITS>
 __global__ void __launch_bounds__(THREADS, RESIDENT<BITS>)
 adamw_kernel(const Tensor* __restrict__ tensors, const int* __restrict__ first, int count, int total, int lg, Clock* clock, double b1,
-             double b2, float eps, double lr, float grad_scale) {
+             double b2, float eps, double lr, float grad_scale, float one) {
   extern __shared__ __align__(128) uint8_t memory[];
   __shared__ Rates rates;
   if (threadIdx.x == 0) {
@@ -473,7 +475,7 @@ adamw_kernel(const Tensor* __restrict__ tensors, const int* __restrict__ first, 
     const long long t = clock->t;
     const auto both = [](double x) { return pair(static_cast<float>(x), static_cast<float>(x)); };
     rates = Rates{both(grad_scale), both(b1), both(1.0 - b1), both(b2), both(1.0 - b2), both(1.0 / sqrt(1.0 - p2)), both(eps),
-                  both(-lr / (1.0 - p1)), static_cast<float>(lr), eps < 1e-12f};
+                  both(-lr / (1.0 - p1)), both(one), static_cast<float>(lr), eps < 1e-12f};
     // the block that comes last has read the clock after every other one, and moves it on
     __threadfence();
     if (atomicAdd(&clock->seen, 1u) == gridDim.x - 1) {
@@ -656,8 +658,8 @@ extern "C" mbd_status mbd_adamw_step(mbd_adamw* opt, double lr, double grad_scal
   const dim3 grid(static_cast<unsigned>(opt->grid)), block(THREADS);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = opt->bits == 32
-      ? launch_pdl(adamw_kernel<32>, grid, block, smem_bytes<32>(), stream, 0, static_cast<const Tensor*>(opt->tensors), static_cast<const int*>(opt->first), opt->count, opt->total, opt->lg, opt->clock, opt->b1, opt->b2, opt->eps, lr, static_cast<float>(grad_scale))
-      : launch_pdl(adamw_kernel<8>, grid, block, smem_bytes<8>(), stream, 0, static_cast<const Tensor*>(opt->tensors), static_cast<const int*>(opt->first), opt->count, opt->total, opt->lg, opt->clock, opt->b1, opt->b2, opt->eps, lr, static_cast<float>(grad_scale));
+      ? launch_pdl(adamw_kernel<32>, grid, block, smem_bytes<32>(), stream, 0, static_cast<const Tensor*>(opt->tensors), static_cast<const int*>(opt->first), opt->count, opt->total, opt->lg, opt->clock, opt->b1, opt->b2, opt->eps, lr, static_cast<float>(grad_scale), 1.f)
+      : launch_pdl(adamw_kernel<8>, grid, block, smem_bytes<8>(), stream, 0, static_cast<const Tensor*>(opt->tensors), static_cast<const int*>(opt->first), opt->count, opt->total, opt->lg, opt->clock, opt->b1, opt->b2, opt->eps, lr, static_cast<float>(grad_scale), 1.f);
   if (e != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_CUDA; }
   return MBD_OK;
 }

@@ -304,3 +304,36 @@ def test_a_very_small_eps_and_very_small_gradients(bits):
     want, _, _ = _step(np.zeros(256), g.double().cpu().numpy(), np.zeros(256), np.zeros(256), 1, 0.01, 0.0, eps=1e-20)
     _near(p.double().cpu().numpy(), want, 1e-4)
     opt.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+def test_moments_are_the_plain_float_formulas_bit_for_bit(grad):
+    # each product and sum in float on the host; the codes by the type's own rounding of the float quotient
+    import torch
+    f = np.float32
+    b1, c1, b2, c2 = f(0.9), f(1.0 - 0.9), f(0.999), f(1.0 - 0.999)
+    for bits in (32, 8):
+        opt = _make([200_000], "bf16+master", grad, bits, seed=9)
+        g = opt.grads[0].float().cpu().numpy() * f(1 / 64)
+        m, v = opt.m[0].float().cpu().numpy(), opt.v[0].float().cpu().numpy()
+        if bits == 8:
+            spread = lambda x: np.repeat(x.cpu().numpy(), BLOCK)[:200_000]  # noqa: E731
+            m, v = m * spread(opt.m_scales[0]), v * spread(opt.v_scales[0])
+            v = v * v
+        m, v = m * b1 + g * c1, v * b2 + (g * g) * c2
+        opt.step(0.01, grad_scale=1 / 64)
+        if bits == 32:
+            assert np.array_equal(opt.m[0].cpu().numpy(), m) and np.array_equal(opt.v[0].cpu().numpy(), v)
+            opt.close()
+            continue
+        for x, held, scales in ((m, opt.m[0], opt.m_scales[0]), (np.sqrt(v), opt.v[0], opt.v_scales[0])):
+            pad = np.zeros(-(-x.size // BLOCK) * BLOCK, f)
+            pad[:x.size] = x
+            s = np.abs(pad.reshape(-1, BLOCK)).max(1) / f(448)
+            assert np.array_equal(scales.cpu().numpy(), s)
+            q = torch.from_numpy((pad.reshape(-1, BLOCK) / s[:, None]).ravel()[:x.size]).cuda()
+            if held is opt.v[0]:
+                q = torch.where(q > 0, q.clamp_min(2.0 ** -9), q)
+            assert torch.equal(held.view(torch.uint8), q.to(torch.float8_e4m3fn).view(torch.uint8))
+        opt.close()
