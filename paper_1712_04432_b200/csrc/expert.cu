@@ -42,13 +42,32 @@ constexpr int SEG_BLOCKS = 64;                // k-blocks per accumulation segme
 
 enum { KIND_BF16 = 0, KIND_I8 = 1 };
 
+// Division of 0 <= n < 2^31 by a number fixed on the host: n * ceil(2^(31 + l) / d) >> (31 + l), 2^(l - 1) < d <= 2^l, which is
+// exact.  (A tile's place took six integer divisions, in every warp's chain from one tile to the next.)
+struct Divisor {
+  uint32_t m = 0;
+  int s = 0;
+  Divisor() = default;
+  explicit Divisor(uint32_t d) {
+    int l = 0;
+    while ((1ull << l) < d) ++l;
+    s = 31 + l;
+    m = static_cast<uint32_t>(((1ull << s) + d - 1) / d);
+  }
+  __device__ __forceinline__ int of(int n) const { return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(n)) * m) >> s); }
+};
+
+constexpr int DIRECT_BELOW = 8;               // k-blocks, see `epilogue`
+constexpr int GROUP_N = 8;                    // row tiles per raster group
+
 struct Params {
   int E, T;                  // experts; rows of the row tensors (offsets are clamped to [0, T])
   const int32_t* offsets;    // [E + 1] on the device, or null: one group of all T rows
   int M, N;                  // output channels; variant 2: output rows per expert (d_out)
   int kb_total;              // variants 0, 1: k-blocks
   int m_tiles, n_tiles;      // n_tiles: variant 2 only
-  int group_n;               // row tiles per raster group
+  int n_step;                // variant 2: rows of a tile
+  Divisor per_expert, per_group, by[GROUP_N];       // variant 2: tiles of an expert; tiles of a raster group; 1 .. GROUP_N
   int chunked_a, chunked_b;  // MN-major operands: the map has chunks of 64 columns as a dimension, one box holds all of a tile's
   int seg;                   // k-blocks per segment: the tensor core truncates when it adds to the accumulator (relative error
                              // ~1.1e-9 per element of K, measured), so a float result is summed from segments of 4096 in
@@ -177,9 +196,10 @@ struct Unit {
 struct Groups {
   int bound[MAX_EXPERTS + 1];
   int first[MAX_EXPERTS + 1];
+  int step[MAX_EXPERTS];     // rows of a tile of expert e
 };
 
-template <int BN>
+template <int B_MN, int BN>
 __device__ __forceinline__ void find_groups(const Params& p, Groups* g, int lane) {
   int top = 0, tiles = 0;
   for (int base = 0; base <= p.E; base += 32) {
@@ -193,13 +213,16 @@ __device__ __forceinline__ void find_groups(const Params& p, Groups* g, int lane
     v = max(v, top);
     int before = __shfl_up_sync(0xffffffffu, v, 1);
     if (lane == 0) before = base == 0 ? v : top;
-    int t = i <= p.E ? (v - before + BN - 1) / BN : 0;          // tiles of expert i - 1
+    const int own = i <= p.E ? (v - before + BN - 1) / BN : 0;  // tiles of expert i - 1
+    int t = own;
     for (int d = 1; d < 32; d <<= 1) {
       const int o = __shfl_up_sync(0xffffffffu, t, d);
       if (lane >= d) t += o;
     }
     t += tiles;
     if (i <= p.E) { g->bound[i] = v; g->first[i] = t; }
+    // the rows of a group are dealt out evenly over its tiles, in steps of 32
+    if (!B_MN && i >= 1 && i <= p.E && own > 0) g->step[i - 1] = ((v - before + own - 1) / own + 31) / 32 * 32;
     top = __shfl_sync(0xffffffffu, v, 31);
     tiles = __shfl_sync(0xffffffffu, t, 31);
   }
@@ -215,29 +238,28 @@ template <int B_MN, int BN, int PAIR>
 __device__ __forceinline__ Unit unit_at(const Params& p, const Groups* g, int w, int& e) {
   constexpr int STEP = B_MN ? (PAIR ? 128 : 64) : 32;
   Unit u;
-  int local, tiles, count;
+  int local, tiles, count, step;
   if (B_MN) {
     tiles = p.n_tiles;
-    const int per = p.m_tiles * tiles;
-    e = w / per;
-    local = w - e * per;
+    e = p.per_expert.of(w);
+    local = w - e * (p.m_tiles * tiles);
     count = p.N;
+    step = p.n_step;
   } else {
     while (w >= g->first[e + 1] * p.m_tiles) ++e;
     local = w - g->first[e] * p.m_tiles;
     tiles = g->first[e + 1] - g->first[e];
     count = g->bound[e + 1] - g->bound[e];
+    step = g->step[e];
   }
-  // raster groups of `group_n` row tiles, row tiles first: the operands of neighbouring units are shared in L2
-  const int per_group = p.group_n * p.m_tiles;
-  const int gi = local / per_group;
-  const int size = min(tiles - gi * p.group_n, p.group_n);
-  const int r = local - gi * per_group;
-  const int tn = gi * p.group_n + r % size;
-  // the rows of a group are dealt out evenly: the instruction's cost per column grows when columns are few
-  const int step = ((count + tiles - 1) / tiles + STEP - 1) / STEP * STEP;
+  // raster groups of GROUP_N row tiles, row tiles first: the operands of neighbouring units are shared in L2
+  const int gi = p.per_group.of(local);
+  const int size = min(tiles - gi * GROUP_N, GROUP_N);
+  const int r = local - gi * (GROUP_N * p.m_tiles);
+  const int mt = p.by[size - 1].of(r);
+  const int tn = gi * GROUP_N + r - mt * size;
   u.e = e;
-  u.m0 = (r / size) * (PAIR ? 2 * CH : CH);
+  u.m0 = mt * (PAIR ? 2 * CH : CH);
   u.row0 = tn * step;
   u.rows = min(step, count - u.row0);
   u.nt = (u.rows + STEP - 1) / STEP * STEP;
@@ -343,14 +365,9 @@ __device__ __forceinline__ void finish(const Params& p, const Unit& u, const uin
   }
 }
 
-// A box of CNT output rows of this warp's 32 channels (float: 16 rows of 128 bytes, bf16: 32 rows of 64 bytes) in staging memory: turned
-// from a channel per lane to rows, so that 16 bytes of a row can leave (and 16 bytes of a mask be met) per lane.  Going to global memory
-// straight from the accumulator's layout cost 24 instructions per element of address and predicate (skewed weight gradients 127
-// against 85 us).  read: the box holds the old weights of
-// Eq. 1 and is combined in place.
+// The accumulators of CNT output rows of a channel, scaled, with bias and ReLU.
 template <int KIND, int CNT>
-__device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const uint32_t* r, int64_t row, int rows, int lane, float bias, float ch_scale, bool read) {
-  float v[CNT];
+__device__ __forceinline__ void values(const Params& p, const uint32_t* r, float* v, int64_t row, int rows, int lane, float bias, float ch_scale) {
   if (KIND == KIND_I8) {
     const float mine = lane < rows ? p.row_scale[row + lane] : 0.f;
 #pragma unroll
@@ -367,6 +384,35 @@ __device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const ui
 #pragma unroll
     for (int j = 0; j < CNT; ++j) v[j] = relu(v[j]);
   }
+}
+
+// 16 float rows straight from the accumulator's layout: a warp stores 32 channels of a row, with nothing to wait for.  `out`: row
+// `row`, channel 0.
+template <int KIND>
+__device__ __forceinline__ void put_rows(const Params& p, const uint32_t* r, float* out, int64_t row, int left, int m, int lane, float bias, float ch_scale) {
+  float v[16];
+  values<KIND, 16>(p, r, v, row, left, lane, bias, ch_scale);
+  if (m >= p.M) return;
+  float* at = out + m;
+  if (left >= 16) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j, at += p.ldo) *at = v[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j, at += p.ldo)
+      if (j < left) *at = v[j];
+  }
+}
+
+// A box of CNT output rows of this warp's 32 channels (float: 16 rows of 128 bytes, bf16: 32 rows of 64 bytes) in staging memory: turned
+// from a channel per lane to rows, so that 16 bytes of a row can leave (and 16 bytes of a mask be met) per lane.  Going to global memory
+// straight from the accumulator's layout cost 24 instructions per element of address and predicate (skewed weight gradients 127
+// against 85 us).  read: the box holds the old weights of
+// Eq. 1 and is combined in place.
+template <int KIND, int CNT>
+__device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const uint32_t* r, int64_t row, int rows, int lane, float bias, float ch_scale, bool read) {
+  float v[CNT];
+  values<KIND, CNT>(p, r, v, row, rows, lane, bias, ch_scale);
   if (CNT == 16) {
     float* at = reinterpret_cast<float*>(box) + lane;
     if (read) {
@@ -428,6 +474,10 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
     // element by element: a sum over segments (it adds to `out`), and an edge that cuts 16 bytes in two
     const bool staged = u.kb <= p.seg && (m0 + 32 <= p.M || p.M % (16 / SIZE) == 0);
     const int plane = B_MN ? u.e : 0;
+    // Float rows of a tile with no main loop to speak of: stores that wait for nothing (skewed weight gradients, a k-block or two a tile:
+    // 82 against 97 us; from 16 k-blocks on the bulk stores, which leave the LSU and the issue slots to the others, are as good or better:
+    // weight gradients of 8 experts 253 against 263 us)
+    const bool direct = CNT == 16 && !sgd && !mask && u.kb < DIRECT_BELOW;
     if (u.kb == 0 && sgd) continue;                          // an expert without rows: nothing to add to its weights
     // this lane's 16 bytes of a box's first rows
     const int ch = m0 + lane % LANES * (16 / SIZE), lr = lane / LANES;
@@ -481,6 +531,10 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
           for (int j = 0; j < CNT; ++j) r[j] = 0;
         }
         const int left = u.rows - b * CNT;
+        if (CNT == 16 && direct) {
+          put_rows<KIND>(p, r, static_cast<float*>(p.out) + u.e * p.out_stride + (u.row0 + b * CNT) * p.ldo, u.row0 + b * CNT, left, m, lane, bias, cs);
+          continue;
+        }
         if (!staged) {
           finish<KIND, CNT>(p, u, r, b * CNT, left, m, lane, bias, cs, kb > 0, last);
           continue;
@@ -610,7 +664,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   }
   pdl_trigger();
   pdl_wait();                              // the offsets may come from the kernel before this one
-  if (warp == 0) find_groups<BN>(p, &groups, lane);
+  if (warp == 0) find_groups<B_MN, BN>(p, &groups, lane);
   tc_fence_before();
   __syncthreads();
   if (PAIR) cluster_sync();                // the other CTA's barriers exist before anything remote touches them (SPLIT meets below)
@@ -1116,7 +1170,14 @@ mbd_status run(Call c) {
   p.kb_total = static_cast<int>((K + per_kb - 1) / per_kb);
   p.m_tiles = static_cast<int>((M + (l.pair ? 2 * CH : CH) - 1) / (l.pair ? 2 * CH : CH));
   p.n_tiles = static_cast<int>((N + l.BN - 1) / l.BN);
-  p.group_n = 8;
+  if (c.variant == 2) {                   // the rows of dW_e are dealt out evenly over its tiles
+    const int unit_rows = l.pair ? 128 : 64;
+    p.n_step = (p.N + p.n_tiles - 1) / p.n_tiles;
+    p.n_step = (p.n_step + unit_rows - 1) / unit_rows * unit_rows;
+    p.per_expert = Divisor(static_cast<uint32_t>(p.m_tiles) * p.n_tiles);
+  }
+  p.per_group = Divisor(static_cast<uint32_t>(GROUP_N) * p.m_tiles);
+  for (int k = 0; k < GROUP_N; ++k) p.by[k] = Divisor(k + 1);
   p.chunked_a = chunked_a; p.chunked_b = chunked_b;
   p.seg = c.kind == KIND_BF16 && !t->out_bf16 && !l.split ? SEG_BLOCKS : 1 << 30;
   p.op = t->op == MBD_TAIL_STORE ? EPI_ACT : t->op == MBD_TAIL_MASK ? EPI_MASK : EPI_SGD;
