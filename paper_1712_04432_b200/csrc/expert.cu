@@ -409,8 +409,7 @@ __device__ __forceinline__ void put_rows(const Params& p, const uint32_t* r, flo
 // A box of CNT output rows of this warp's 32 channels (float: 16 rows of 128 bytes, bf16: 32 rows of 64 bytes) in staging memory: turned
 // from a channel per lane to rows, so that 16 bytes of a row can leave (and 16 bytes of a mask be met) per lane.  Going to global memory
 // straight from the accumulator's layout cost 24 instructions per element of address and predicate (skewed weight gradients 127
-// against 85 us).  read: the box holds the old weights of
-// Eq. 1 and is combined in place.
+// against 85 us).  read: the box holds the old weights of Eq. 1 and is combined in place.
 template <int KIND, int CNT>
 __device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const uint32_t* r, int64_t row, int rows, int lane, float bias, float ch_scale, bool read) {
   float v[CNT];
@@ -465,7 +464,7 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
   constexpr int SIZE = CNT == 32 ? 2 : 4, LANES = 32 * SIZE / 16, ROWS = 32 / LANES;      // lanes per row, rows per access
   const bool sgd = p.op == EPI_SGD, mask = p.op == EPI_MASK && p.mask != nullptr;
   int it = 0, expert = 0;
-  uint32_t n = 0, phases = 0;              // SGD: boxes so far modulo BOXES, and the parity of each box's barrier
+  uint32_t n = 0, phases = 0;              // boxes so far modulo BOXES; SGD: the parity of each box's barrier
   bool ok = true;
   for (int w = w_first; w < total && ok; w += w_step) {
     const Unit u = unit_at<B_MN, BN, PAIR>(p, groups, w, expert);
