@@ -554,6 +554,22 @@ def softmax_xent(logits, labels, dY, per_sample, sync: bool = True):
                                   _ptr(per_sample), int(sync), _stream()), "mbd_softmax_xent")
 
 
+# What the calls below use of torch at every launch, looked up once: their host time is a good part of a small product's.
+_t = None
+
+
+def _torch():
+    global _t
+    if _t is None:
+        import types
+
+        import torch
+        torch.cuda.init()
+        _t = types.SimpleNamespace(bf16=torch.bfloat16, f32=torch.float32, i32=torch.int32, i8=torch.int8,
+                                   device=torch._C._cuda_getDevice, stream=torch._C._cuda_getCurrentRawStream)
+    return _t
+
+
 def _at(t, dev: int) -> int:
     """Address of a tensor on the current device, where the call's stream is."""
     assert t.get_device() == dev, "tensors lie on the current CUDA device"
@@ -566,37 +582,38 @@ def _at_or_none(t, dev: int):
 
 def _word(status, dev: int):
     """Address of a caller's status word, or None."""
-    import torch
-    assert status is None or status.dtype == torch.int32
-    return _at_or_none(status, dev)
+    if status is None:
+        return None
+    assert status.dtype == _t.i32
+    return _at(status, dev)
 
 
-def _ld(t, shape, stride) -> int:
+def _ld(t, shape) -> int:
     """Elements between rows.  A tensor of one row (or none) has no meaningful stride: the row rounded up to what the library asks for."""
+    stride = t.stride()
     assert stride[-1] == 1 or shape[-1] == 1
     return stride[-2] if shape[-2] > 1 else (shape[-1] + 15) // 16 * 16
 
 
 def _group_tail(op: int, out, out_shape, dev: int, relu: bool, bias, bias_shape, mask, scale: float) -> Tail:
-    import torch
     dt = out.dtype
-    assert dt in (torch.bfloat16, torch.float32) and out.shape == out_shape
-    t = Tail(op, dt == torch.bfloat16, relu, 0, _at(out, dev), _ld(out, out_shape, out.stride()), None, None, 0, scale)
+    assert (dt == _t.bf16 or dt == _t.f32) and out.shape == out_shape
+    t = Tail(op, dt == _t.bf16, relu, 0, _at(out, dev), _ld(out, out_shape), None, None, 0, scale)
     if bias is not None:
-        assert bias.dtype == torch.float32 and bias.shape == bias_shape and bias.is_contiguous()
+        assert bias.dtype == _t.f32 and bias.shape == bias_shape and bias.is_contiguous()
         t.bias_dev = _at(bias, dev)
     if mask is not None:
         assert mask.dtype == dt and mask.shape == out_shape
         t.mask_dev = _at(mask, dev)
-        t.ldmask = _ld(mask, out_shape, mask.stride())
+        t.ldmask = _ld(mask, out_shape)
     return t
 
 
 def _device():
     """The current device and its current stream."""
-    import torch
-    dev = torch.cuda.current_device()
-    return dev, torch._C._cuda_getCurrentRawStream(dev)
+    t = _t or _torch()
+    dev = t.device()
+    return dev, t.stream(dev)
 
 
 def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bool = False, bias=None, mask=None,
@@ -608,10 +625,9 @@ def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bo
       variant 2: A = dY [T, d_out], B = X [T, d_in], out [E, d_out, d_in], op TAIL_SGD with scale
     bf16 operands with free row strides (multiples of 8), `out` bf16 or float; `mask` in out's type.  Rows of `out` in no group
     stay as they are.  `status` (int32 CUDA tensor of one zero): enqueue only; otherwise the call waits for the stream."""
-    import torch
     dev, stream = _device()
     sa, sb, so = A.shape, B.shape, offsets.shape
-    assert A.dtype == torch.bfloat16 and B.dtype == torch.bfloat16 and offsets.dtype == torch.int32
+    assert A.dtype == _t.bf16 and B.dtype == _t.bf16 and offsets.dtype == _t.i32
     assert len(sa) == 2 and len(so) == 1 and so[0] >= 2 and offsets.stride(0) == 1
     E, T = so[0] - 1, sa[0]
     if variant == 2:
@@ -624,8 +640,8 @@ def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bo
         assert sa[1] == (d_out if variant else d_in)
         shape, stacked = (T, d_in if variant else d_out), B
     t = _group_tail(op, out, shape, dev, relu, bias, (E, d_out), mask, scale)
-    _check(lib().mbd_expert_gemm_bf16(variant, E, _at(offsets, dev), T, d_out, d_in, _at(A, dev), _ld(A, sa, A.stride()), _at(B, dev),
-                                      _ld(B, sb, B.stride()), stacked.stride(0), C.byref(t), _word(status, dev), stream),
+    _check(lib().mbd_expert_gemm_bf16(variant, E, _at(offsets, dev), T, d_out, d_in, _at(A, dev), _ld(A, sa), _at(B, dev),
+                                      _ld(B, sb), stacked.stride(0), C.byref(t), _word(status, dev), stream),
            "mbd_expert_gemm_bf16")
     return out
 
@@ -633,14 +649,13 @@ def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bo
 def quantize_rows(X, q, scale, sync: bool = False):
     """mbd_quantize_rows: X [.., K] (bf16 or float; all but the last dimension are rows) to q (int8, same shape) and scale (float [..]):
     scale = max |row| / 127, q = row / scale correctly rounded.  Enqueues only unless `sync`."""
-    import torch
     dev, stream = _device()
-    shape = X.shape
-    assert X.dtype in (torch.bfloat16, torch.float32) and q.dtype == torch.int8 and scale.dtype == torch.float32
+    shape, dt = X.shape, X.dtype
+    assert (dt == _t.bf16 or dt == _t.f32) and q.dtype == _t.i8 and scale.dtype == _t.f32
     assert len(shape) >= 1 and q.shape == shape and scale.shape == shape[:-1] and scale.is_contiguous()
     (rows, K), ldx = _as_rows(X, shape)
     _, ldq = _as_rows(q, shape)
-    _check(lib().mbd_quantize_rows(_at(X, dev), X.dtype == torch.bfloat16, rows, K, ldx, _at(q, dev), ldq, _at(scale, dev), sync, stream),
+    _check(lib().mbd_quantize_rows(_at(X, dev), dt == _t.bf16, rows, K, ldx, _at(q, dev), ldq, _at(scale, dev), sync, stream),
            "mbd_quantize_rows")
     return q, scale
 
@@ -651,19 +666,18 @@ def _as_rows(t, shape):
         t = t.view(-1, shape[-1])
         shape = t.shape
     rows, K = shape
-    stride = t.stride()
-    assert K == 1 or stride[1] == 1
-    return (rows, K), (max(stride[0], K) if rows > 1 else K)
+    ld, one = t.stride()
+    assert K == 1 or one == 1
+    return shape, (ld if rows > 1 else K)
 
 
 def _i8(A, a_scale, B, b_scale, out, relu, bias, dev):
-    import torch
     sa, sb = A.shape, B.shape
-    assert A.dtype == torch.int8 and B.dtype == torch.int8 and len(sa) == 2 and sb[-1] == sa[1]
-    assert a_scale.dtype == torch.float32 and a_scale.shape == sa[:1] and a_scale.is_contiguous()
-    assert b_scale.dtype == torch.float32 and b_scale.shape == sb[:-1] and b_scale.is_contiguous()
+    assert A.dtype == _t.i8 and B.dtype == _t.i8 and len(sa) == 2 and len(sb) >= 2 and sb[-1] == sa[1]
+    assert a_scale.dtype == _t.f32 and a_scale.shape == sa[:1] and a_scale.is_contiguous()
+    assert b_scale.dtype == _t.f32 and b_scale.shape == sb[:-1] and b_scale.is_contiguous()
     t = _group_tail(TAIL_STORE, out, (sa[0], sb[-2]), dev, relu, bias, sb[:-1], None, 0.0)
-    return sa, sb, _ld(A, sa, A.stride()), _ld(B, sb, B.stride()), t
+    return sa, sb, _ld(A, sa), _ld(B, sb), t
 
 
 def gemm_i8(A, a_scale, B, b_scale, out, relu: bool = False, bias=None, status=None):
@@ -680,10 +694,9 @@ def gemm_i8(A, a_scale, B, b_scale, out, relu: bool = False, bias=None, status=N
 def expert_gemm_i8(A, a_scale, B, b_scale, offsets, out, relu: bool = False, bias=None, status=None):
     """mbd_expert_gemm_i8: gemm_i8 grouped by expert: B [E, d_out, d_in], b_scale and bias [E, d_out]; rows and offsets as in
     expert_gemm."""
-    import torch
     dev, stream = _device()
     sa, sb, lda, ldb, t = _i8(A, a_scale, B, b_scale, out, relu, bias, dev)
-    assert len(sb) == 3 and offsets.dtype == torch.int32 and offsets.is_contiguous() and offsets.shape == (sb[0] + 1,)
+    assert len(sb) == 3 and offsets.dtype == _t.i32 and offsets.is_contiguous() and offsets.shape == (sb[0] + 1,)
     _check(lib().mbd_expert_gemm_i8(sb[0], _at(offsets, dev), sa[0], sb[1], sb[2], _at(A, dev), lda, _at(a_scale, dev), _at(B, dev), ldb,
                                     B.stride(0), _at(b_scale, dev), C.byref(t), _word(status, dev), stream), "mbd_expert_gemm_i8")
     return out
@@ -715,7 +728,7 @@ class AdamW:
         lists = (self.grads, self.masters, self.m, self.v, self.m_scales, self.v_scales, decay)
         assert all(len(x) == n for x in lists)
         table = (AdamWTensor * max(n, 1))()
-        dev = torch.cuda.current_device()
+        dev, _ = _device()
         at = lambda x: _at_or_none(x, dev)  # noqa: E731
         for i, (p, g, w, a, b, sa, sb, wd) in enumerate(zip(self.params, *lists)):
             assert p.dtype in (torch.float32, torch.bfloat16) and g.dtype in (torch.float32, torch.bfloat16)

@@ -249,3 +249,22 @@ def test_captured_and_replayed():
         ref = (q.double() @ B.double().T) * s.double()[:, None] * sb.double()
         _close(out, ref, torch.float32, ref.abs())
     assert int(status) == 0
+
+
+@pytest.mark.gpu
+def test_the_binding_refuses_what_it_would_misread():
+    import torch
+    X, q, s = torch.randn(4, 32, device="cuda"), torch.empty(4, 32, dtype=torch.int8, device="cuda"), torch.empty(4, device="cuda")
+    mbd.quantize_rows(X, q, s)
+    for bad in ((X.t(), q.t(), torch.empty(32, device="cuda")), (X.half(), q, s), (X, q, s[:2]), (X, q.short(), s), (X.cpu(), q, s), (X[:2], q, s), (X, q, s.double())):
+        with pytest.raises(AssertionError):
+            mbd.quantize_rows(*bad)
+    with pytest.raises(mbd.MbdError) as e:
+        mbd.quantize_rows(X[:1].expand(4, 32), q, s)                # rows on top of each other
+    assert e.value.status == mbd.E_INVALID
+    B, sb, out = torch.zeros(8, 32, dtype=torch.int8, device="cuda"), torch.ones(8, device="cuda"), torch.empty(4, 8, device="cuda")
+    mbd.gemm_i8(q, s, B, sb, out)
+    for bad in (dict(A=X), dict(B=B[None]), dict(B=B[:, :16]), dict(a_scale=s[:3]), dict(b_scale=sb[:4]), dict(out=out.t()), dict(out=out.half()), dict(bias=sb[:4]),
+                dict(status=s)):
+        with pytest.raises(AssertionError):
+            mbd.gemm_i8(**{**dict(A=q, a_scale=s, B=B, b_scale=sb, out=out), **bad})
