@@ -470,32 +470,30 @@ adamw_kernel(const Tensor* __restrict__ tensors, const int* __restrict__ first, 
              double b2, float eps, double lr, float grad_scale, float one) {
   extern __shared__ __align__(128) uint8_t memory[];
   __shared__ Rates rates;
-  if (threadIdx.x == 0) {
-    const double p1 = clock->b1_t * b1, p2 = clock->b2_t * b2;
-    const long long t = clock->t;
-    const auto both = [](double x) { return pair(static_cast<float>(x), static_cast<float>(x)); };
-    rates = Rates{both(grad_scale), both(b1), both(1.0 - b1), both(b2), both(1.0 - b2), both(1.0 / sqrt(1.0 - p2)), both(eps),
-                  both(-lr / (1.0 - p1)), both(one), static_cast<float>(lr), eps < 1e-12f};
-    // the block that comes last has read the clock after every other one, and moves it on
-    __threadfence();
-    if (atomicAdd(&clock->seen, 1u) == gridDim.x - 1) {
-      clock->b1_t = p1; clock->b2_t = p2; clock->t = t + 1;
-      clock->seen = 0;
-    }
-  }
-  __syncthreads();
   const int lane = threadIdx.x & 31;
   const uint8_t* my = memory + (threadIdx.x >> 5) * DEPTH * STAGE_BYTES<BITS>;
   const int lo = static_cast<int>(static_cast<long long>(blockIdx.x) * total / gridDim.x);
   const int hi = static_cast<int>(static_cast<long long>(blockIdx.x + 1) * total / gridDim.x);
   int c = lo + (threadIdx.x >> 5);     // this warp's next chunk
-  if (c >= hi) return;
-  int t = 0;                           // the tensor of chunk c: the last one that starts at or before it
-  for (int d = 1 << 30; d; d >>= 1)
-    if (t + d < count && first[t + d] <= c) t += d;
-  for (; c < hi; ++t) {
+  if (threadIdx.x == 0) {
+    const double p1 = clock->b1_t * b1, p2 = clock->b2_t * b2;
+    const auto both = [](double x) { return pair(static_cast<float>(x), static_cast<float>(x)); };
+    rates = Rates{both(grad_scale), both(b1), both(1.0 - b1), both(b2), both(1.0 - b2), both(1.0 / sqrt(1.0 - p2)), both(eps),
+                  both(-lr / (1.0 - p1)), both(one), static_cast<float>(lr), eps < 1e-12f};
+  }
+  // the tensor of chunk c: the last one that starts at or before it; every lane looks at a 32nd of what is left
+  int t = 0;
+  for (int left = count; left > 1;) {
+    const int part = (left + 31) / 32, i = t + lane * part;
+    const bool before = lane * part < left && first[i] <= c;
+    const int last = 31 - __clz(__ballot_sync(0xffffffffu, before) | 1u);
+    t += last * part;
+    left = min(part, left - last * part);
+  }
+  __syncthreads();
+  while (c < hi) {
     const int start = first[t], end = min(first[t + 1], hi);
-    if (c >= end) continue;
+    if (c >= end) { ++t; continue; }
     const Tensor w = tensors[t];
     const uint32_t c0 = c - start, stop = end - start;
     uint32_t blocks;
@@ -508,6 +506,15 @@ adamw_kernel(const Tensor* __restrict__ tensors, const int* __restrict__ first, 
       default: blocks = share<BITS, P_BF16 | G_BF16 | MASTERED>(w, c0, stop, lg, my, lane, rates); break;
     }
     c += ((blocks + (1u << lg) - 1u) >> lg) * WARPS;       // (the first chunk of this warp's at or behind `end`)
+    ++t;
+  }
+  // the block that comes here last moves the clock on: every other one has read it long ago
+  if (threadIdx.x == 0) {
+    __threadfence();
+    if (atomicAdd(&clock->seen, 1u) == gridDim.x - 1) {
+      clock->b1_t *= b1; clock->b2_t *= b2; clock->t += 1;
+      clock->seen = 0;
+    }
   }
 }
 
