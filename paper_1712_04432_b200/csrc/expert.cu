@@ -560,10 +560,17 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
           // by one bulk store where the whole box is this group's; with a mask, or at a group's last rows (those behind them are another
           // group's), by 16 bytes a lane.  (All boxes that way: weight gradients 282 against 251 us, the stores share the issue slots of
           // the warps.  Masks by bulk copies: backward-data 80 against 73 us, they queue behind the operands' copies.)
-          const bool bulk = !mask && (B_MN || left >= CNT);
+          const bool bulk = B_MN || left >= CNT;
           if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(BOXES - 1) : "memory");      // the store that used this box has read it
           __syncwarp();
           fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, left, lane, bias, cs, false);
+          if (mask) {
+            __syncwarp();
+            uint4* const at = reinterpret_cast<uint4*>(box) + lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) at[i * 32] = masked<CNT>(at[i * 32], mk[i]);
+            if (b + 2 < count) load_mask(b + 2);
+          }
           if (bulk) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -574,11 +581,6 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
             uint4 v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint4*>(box + i * 512 + lane * 16);
-            if (mask) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) v[i] = masked<CNT>(v[i], mk[i]);
-              if (b + 2 < count) load_mask(b + 2);
-            }
             char* at = out + b * CNT * p.ldo * SIZE;
 #pragma unroll
             for (int i = 0; i < 4; ++i, at += ROWS * p.ldo * SIZE)
