@@ -409,16 +409,20 @@ __device__ __forceinline__ void put_rows(const Params& p, const uint32_t* r, flo
 // A box of CNT output rows of this warp's 32 channels (float: 16 rows of 128 bytes, bf16: 32 rows of 64 bytes) in staging memory: turned
 // from a channel per lane to rows, so that 16 bytes of a row can leave (and 16 bytes of a mask be met) per lane.  Going to global memory
 // straight from the accumulator's layout cost 24 instructions per element of address and predicate (skewed weight gradients 127
-// against 85 us).  read: the box holds the old weights of Eq. 1 and is combined in place.
+// against 85 us).  met: the box holds the old weights of Eq. 1 or a mask and is combined in place.
+enum Met { NOTHING, OLD_WEIGHTS, MASK };
 template <int KIND, int CNT>
-__device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const uint32_t* r, int64_t row, int rows, int lane, float bias, float ch_scale, bool read) {
+__device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const uint32_t* r, int64_t row, int rows, int lane, float bias, float ch_scale, Met met) {
   float v[CNT];
   values<KIND, CNT>(p, r, v, row, rows, lane, bias, ch_scale);
   if (CNT == 16) {
     float* at = reinterpret_cast<float*>(box) + lane;
-    if (read) {
+    if (met == OLD_WEIGHTS) {
 #pragma unroll
       for (int j = 0; j < CNT; ++j) v[j] = fmaf(p.scale, v[j], at[j * 32]);
+    } else if (met == MASK) {
+#pragma unroll
+      for (int j = 0; j < CNT; ++j) v[j] = at[j * 32] > 0.f ? v[j] : 0.f;
     }
 #pragma unroll
     for (int j = 0; j < CNT; ++j) at[j * 32] = v[j];
@@ -427,7 +431,7 @@ __device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const ui
     const int odd = lane & 1;
     uint32_t* at = reinterpret_cast<uint32_t*>(box) + odd * 16 + (lane >> 1);
     uint32_t w[CNT / 2];
-    if (read) {
+    if (met != NOTHING) {
 #pragma unroll
       for (int j = 0; j < CNT / 2; ++j) w[j] = at[j * 32];
     }
@@ -435,25 +439,16 @@ __device__ __forceinline__ void fill_box(const Params& p, uint8_t* box, const ui
     for (int j = 0; j < CNT / 2; ++j) {
       const float got = __shfl_xor_sync(0xffffffffu, odd ? v[2 * j] : v[2 * j + 1], 1);
       float lo = odd ? got : v[2 * j], hi = odd ? v[2 * j + 1] : got;
-      if (read) {
+      if (met == OLD_WEIGHTS) {
         const float xl = bf16_bits_to_f32(w[j] & 0xFFFFu), xh = bf16_bits_to_f32(w[j] >> 16);
         lo = fmaf(p.scale, lo, xl);
         hi = fmaf(p.scale, hi, xh);
       }
-      at[j * 32] = pack_bf16x2(lo, hi);
+      uint32_t both = pack_bf16x2(lo, hi);
+      if (met == MASK) both &= __hgt2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[j]), __float2bfloat162_rn(0.f));
+      at[j * 32] = both;
     }
   }
-}
-
-// 16 bytes of results, where the mask (of the same place) is positive.
-template <int CNT>
-__device__ __forceinline__ uint4 masked(const uint4& v, const uint4& mask) {
-  const auto keep = [](uint32_t x, uint32_t m) {
-    if (CNT == 16) return __uint_as_float(m) > 0.f ? x : 0u;
-    const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
-    return x & __hgt2_mask(*reinterpret_cast<const __nv_bfloat162*>(&m), zero);
-  };
-  return make_uint4(keep(v.x, mask.x), keep(v.y, mask.y), keep(v.z, mask.z), keep(v.w, mask.w));
 }
 
 // The epilogue of one warp: 32 channels (a quarter of the CTA's lanes) of every second box of CNT output rows.
@@ -485,13 +480,21 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
     const bool column = ch < p.M;
     char* const out = reinterpret_cast<char*>(p.out) + (u.e * p.out_stride + (u.row0 + lr) * p.ldo + ch) * SIZE;
     const char* const mask_at = reinterpret_cast<const char*>(p.mask) + ((u.row0 + lr) * p.ldmask + ch) * SIZE;
-    uint4 mk[4];
-    auto load_mask = [&](int b) {
+    // A mask arrives by 16 bytes a lane straight into the boxes, zeros beyond the group, two boxes early.  5003 rows of 16 groups, 4096
+    // channels, K = 64 and 1000: 33 and 53 us (27 and 49 without a mask).  By loads into registers a box early 44 and 59 us: a latency
+    // under load of 1.8 us per box; two boxes early in twice the registers 52 and 66.  By bulk copies it queues behind the operands'.
+    auto fetch = [&](int b, uint32_t at) {
+      if (b < count) {
+        const uint32_t to = smem_u32(boxes) + at * BOX_BYTES + lane * 16;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = b * CNT + i * ROWS;
-        mk[i] = column && row + lr < u.rows ? *reinterpret_cast<const uint4*>(mask_at + row * p.ldmask * SIZE) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+          const int row = b * CNT + i * ROWS;
+          const bool there = column && row + lr < u.rows;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + i * 512),
+                       "l"(there ? mask_at + row * p.ldmask * SIZE : static_cast<const char*>(p.mask)), "r"(there ? 16 : 0) : "memory");
+        }
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
     };
     // the old weights arrive by bulk copies
     auto request = [&](int b, uint32_t at) {                 // lane 0
@@ -500,11 +503,16 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
       load_3d(smem_u32(boxes) + at * BOX_BYTES, tmOut, m0, u.row0 + b * CNT, u.e, bar);
     };
     if (sgd && staged && lane == 0) {
-      asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");             // the last store is that of the third box
       if (half < count) request(half, n);
       if (half + 2 < count) request(half + 2, n + 1 == BOXES ? 0 : n + 1);
     }
-    if (mask && staged && half < count) load_mask(half);     // its latency passes under the tile's products
+    if (mask && staged) {                                    // (the latency of the first two passes under the tile's products)
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+      __syncwarp();
+      fetch(half, n);
+      fetch(half + 2, n + 1 == BOXES ? 0 : n + 1);
+    }
     for (int kb = 0; (kb < u.kb || kb == 0) && ok; kb += p.seg) {
       const bool last = kb + p.seg >= u.kb, some = u.kb > 0; // an expert without rows has a gradient of zeros and no accumulator
       const int acc = it & 1;
@@ -546,7 +554,7 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           phases ^= 1u << n;
-          fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, left, lane, bias, cs, true);
+          fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, left, lane, bias, cs, OLD_WEIGHTS);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
@@ -557,20 +565,15 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
             }
           }
         } else {
-          // by one bulk store where the whole box is this group's; with a mask, or at a group's last rows (those behind them are another
-          // group's), by 16 bytes a lane.  (All boxes that way: weight gradients 282 against 251 us, the stores share the issue slots of
-          // the warps.  Masks by bulk copies: backward-data 80 against 73 us, they queue behind the operands' copies.)
+          // by one bulk store where the whole box is this group's; at a group's last rows (those behind them are another group's) by
+          // 16 bytes a lane.  (All boxes that way: weight gradients 282 against 251 us, the stores share the issue slots of the warps.)
           const bool bulk = B_MN || left >= CNT;
-          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(BOXES - 1) : "memory");      // the store that used this box has read it
+          if (mask) asm volatile("cp.async.wait_group 1;" ::: "memory");                                     // all but the next box's
+          else if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(BOXES - 1) : "memory"); // the store that used this box has read it
           __syncwarp();
-          fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, left, lane, bias, cs, false);
-          if (mask) {
-            __syncwarp();
-            uint4* const at = reinterpret_cast<uint4*>(box) + lane;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) at[i * 32] = masked<CNT>(at[i * 32], mk[i]);
-            if (b + 2 < count) load_mask(b + 2);
-          }
+          // (two calls, each of them straight code: one with a run-time choice cost results without a mask 2 us in 28)
+          if (mask) fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, left, lane, bias, cs, MASK);
+          else fill_box<KIND, CNT>(p, box, r, u.row0 + b * CNT, left, lane, bias, cs, NOTHING);
           if (bulk) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -586,6 +589,11 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
             for (int i = 0; i < 4; ++i, at += ROWS * p.ldo * SIZE)
               if (column && lr + i * ROWS < left) *reinterpret_cast<uint4*>(at) = v[i];
           }
+          if (mask) {                                        // two boxes on: into the box before this one, once its store has read it
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            __syncwarp();
+            fetch(b + 4, n == 0 ? BOXES - 1 : n - 1);
+          }
         }
         if (++n == BOXES) n = 0;
       }
@@ -595,7 +603,8 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
       }
     }
   }
-  if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // stores done before the CTA exits
+  asm volatile("cp.async.wait_all;" ::: "memory");                               // copies and stores done before the CTA exits
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   __syncwarp();
 }
 
