@@ -15,8 +15,8 @@
 // One persistent CTA (or CTA pair, cta_group::2: 256 channels x up to 256 rows, each CTA loads its 128 channels and half
 // of the rows) per SM; warp roles as in the dense kernel: 0 TMA producer, 1 MMA issuer, 2..9 epilogue, and for
 // variant 2 a warp 10 that clears what the last k-block of a group holds of the next group (see `fixer`).
-// Measured (one B200, in a graph): 8 experts, 8192 rows, 4096 -> 4096 forward 0.214 ms (1.28 PFLOP/s; the dense kernel 1.5 on one
-// matrix), their weight gradients in float 0.252 ms (1.09 PFLOP/s: with both operands MN-major a k-block takes 0.43 us instead of
+// Measured (one B200, in a graph): 8 experts, 8192 rows, 4096 -> 4096 forward 0.209 ms (1.31 PFLOP/s; the dense kernel 1.5 on one
+// matrix), their weight gradients in float 0.245 ms (1.12 PFLOP/s: with both operands MN-major a k-block takes 0.43 us instead of
 // 0.33, in the dense kernel as well); 16 tokens over 64 experts of 1024 -> 4096 41 us (5.2 TB/s); int8 8192^3 0.315 ms (3.5 Pop/s).
 // The split form cuts K over the CTAs of a cluster and joins the pieces through distributed shared memory, for calls
 // with too few tiles to keep the SMs busy.
