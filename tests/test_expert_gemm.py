@@ -401,3 +401,34 @@ def test_the_binding_refuses_what_it_would_misread():
     with pytest.raises(mbd.MbdError) as e:
         call(A=torch.zeros(8, 20, dtype=torch.bfloat16, device="cuda")[:, :16])          # rows 40 bytes apart
     assert e.value.status == mbd.E_UNSUPPORTED
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bfloat16", "float32"])
+@pytest.mark.parametrize("d_in", [2056, 100, 4096])
+@pytest.mark.parametrize("d_out", [64, 1000])
+def test_masks_over_many_boxes_are_the_product_where_positive(kind, d_in, d_out):
+    """Tiles of up to eight boxes, many tiles per SM, groups that end inside a box, empty groups; the mask in rows of its own stride, and in
+    the result's own memory.  The sums do not depend on the mask: every element is the unmasked one or zero, bit for bit."""
+    import torch
+    dt = getattr(torch, kind)
+    gen = torch.Generator(device="cuda").manual_seed(d_in + d_out)
+    counts = [0, 1, 255, 256, 257, 0, 700, 33, 1031, 31, 513, 2, 0]
+    T, E = sum(counts), len(counts)
+    offsets = torch.tensor([0] + counts).cumsum(0).int().cuda()
+    ld = (d_in + 7) // 8 * 8
+    dY = torch.randn(T, d_out, device="cuda", generator=gen).bfloat16()
+    W = torch.randn(E, d_out, ld, device="cuda", generator=gen).bfloat16()[:, :, :d_in]
+    mask = torch.randn(T, ld + 16, device="cuda", generator=gen).to(dt)[:, :d_in]
+    plain = torch.full((T, ld), 7.0, device="cuda", dtype=dt)
+    mbd.expert_gemm(1, dY, W, offsets, plain[:, :d_in])
+    want = torch.where(mask > 0, plain[:, :d_in], torch.zeros((), device="cuda", dtype=dt))
+    out = torch.full((T + 3, ld), 7.0, device="cuda", dtype=dt)
+    for _ in range(3):
+        out[:, :] = 7.0
+        mbd.expert_gemm(1, dY, W, offsets, out[:T, :d_in], op=mbd.TAIL_MASK, mask=mask)
+        assert torch.equal(out[:T, :d_in], want)
+        assert (out[T:] == 7.0).all() and (out[:, d_in:] == 7.0).all()
+    out[:T, :d_in] = mask
+    mbd.expert_gemm(1, dY, W, offsets, out[:T, :d_in], op=mbd.TAIL_MASK, mask=out[:T, :d_in])
+    assert torch.equal(out[:T, :d_in], want)
