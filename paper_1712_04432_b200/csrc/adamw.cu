@@ -277,7 +277,7 @@ __device__ __forceinline__ void request(uint32_t stage, const Place& at, uint32_
   }
   if (BITS == 32) {
     copy16(to + 2048, at.m + b32); copy16(to + 2560, at.m + b32 + 512);
-    copy16(to + 3072, at.v + b32); copy16(to + 3584, at.v + b32 + 512);
+    copy16(to + 3 * 1024, at.v + b32); copy16(to + 3584, at.v + b32 + 512);
   } else {                             // the codes of m by the first 16 lanes, those of v by the others
     copy16(to + 2048, (lane < 16 ? at.m : at.v) + block * uint64_t(256) + 16 * (lane & 15));
   }
@@ -301,7 +301,7 @@ __device__ __forceinline__ void take(Raw<BITS>& r, const uint8_t* stage, int lan
     }
     if (BITS == 32) {
       r.m[h] = *reinterpret_cast<const uint4*>(stage + 2048 + 512 * h + 16 * lane);
-      r.v[h] = *reinterpret_cast<const uint4*>(stage + 3072 + 512 * h + 16 * lane);
+      r.v[h] = *reinterpret_cast<const uint4*>(stage + 3 * 1024 + 512 * h + 16 * lane);
     } else {
       (h ? r.m[0].y : r.m[0].x) = *reinterpret_cast<const uint32_t*>(stage + 2048 + 128 * h + 4 * lane);
       (h ? r.v[0].y : r.v[0].x) = *reinterpret_cast<const uint32_t*>(stage + 2304 + 128 * h + 4 * lane);
