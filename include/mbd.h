@@ -448,11 +448,13 @@ MBD_API mbd_status mbd_softmax_xent(const float* logits_dev, int64_t B, int64_t 
  * tensor core truncates as it accumulates, about 1.1e-9 relative per element of K; a bf16 result is accumulated in one piece).
  * A group may be empty and any length; variant 2 writes zeros for an empty one.  Rows of `out` outside every group (before offsets[0],
  * from offsets[E] on) are left as they are.  Offsets are clamped to [0, T] and a falling one counts as the largest before it, so
- * whatever they hold nothing outside the buffers is touched.  `out` overlaps no operand.  Rows of different groups never meet in a sum: infinities or NaN in
+ * whatever they hold nothing outside the buffers is touched.  `out` overlaps neither A nor B.  Rows of different groups never meet in a sum: infinities or NaN in
  * one group's rows, or in rows of no group, stay out of the others' results.
  * tail: out_dev, ldo, out_bf16 as in mbd_block_gemm_bf16; MBD_TAIL_STORE with bias_dev ([E][d_out] float, dense) and relu
  * for variant 0; MBD_TAIL_MASK with mask_dev ([T, ldmask] in out's type) for variant 1; MBD_TAIL_SGD (out += scale * dW, Eq. 1)
- * for variant 2; MBD_E_UNSUPPORTED for the others.  ReLU keeps a NaN.
+ * for variant 2; MBD_E_UNSUPPORTED for the others.  ReLU keeps a NaN.  The mask may be the result's own memory (the same address and
+ * leading dimension: an activation that its gradient replaces) or share no element with it; MBD_E_INVALID for the two laid over each
+ * other in another way.
  * expert_stride: elements between the experts of W (variants 0, 1) or of dW (variant 2); not read for E = 1.
  * d_in, d_out and T are free (T = 0: a tensor of no rows may be null); leading dimensions and expert_stride are multiples of 8, bases
  * 16-byte aligned, E <= 512 (MBD_E_UNSUPPORTED otherwise, nothing is launched).  MBD_E_INVALID for leading dimensions or an

@@ -342,18 +342,22 @@ __device__ __forceinline__ void finish(const Params& p, const Unit& u, const uin
   float* out = reinterpret_cast<float*>(p.out) + u.e * p.out_stride + base * p.ldo + m;
   const bool here = m < p.M;
   const bool masked = p.op == EPI_MASK && p.mask != nullptr;
-  if (p.op == EPI_SGD || again || (masked && last)) {
+  if (p.op == EPI_SGD || again || masked) {
+    // A mask over several segments is met by the first one, which may find it in the memory that it writes.  What the mask closes
+    // is left as -0 for the segments to come: an open sum is never -0, it starts as a sum with +0 (and x + v is -0 for x = v = -0 only).
+    constexpr uint32_t CLOSED = 0x80000000u;
     float x[CNT], w[CNT];
     const float* mask = reinterpret_cast<const float*>(p.mask) + base * p.ldmask + m;
 #pragma unroll
     for (int j = 0; j < CNT; ++j) {
       x[j] = here && j < rows && (p.op == EPI_SGD || again) ? out[j * p.ldo] : 0.f;
-      w[j] = here && j < rows && masked && last ? mask[j * p.ldmask] : 1.f;
+      w[j] = here && j < rows && masked && !again ? mask[j * p.ldmask] : 1.f;
     }
 #pragma unroll
     for (int j = 0; j < CNT; ++j) {
+      const bool open = w[j] > 0.f && !(masked && __float_as_uint(x[j]) == CLOSED);
       if (p.op == EPI_SGD) v[j] = fmaf(p.scale, v[j], x[j]);
-      else v[j] = w[j] > 0.f ? x[j] + v[j] : 0.f;
+      else v[j] = open ? x[j] + v[j] : last ? 0.f : __uint_as_float(CLOSED);
     }
   }
   if (!here) return;
@@ -1086,6 +1090,18 @@ Launch plan(int kind, int variant, int E, int64_t T, int64_t M, int64_t N, int64
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// A mask is the result's own memory, element on element, or shares none with it: anything else would be met half written.
+bool mask_apart(const mbd_tail& t, int64_t T, int64_t M) {
+  const int64_t size = t.out_bf16 ? 2 : 4, ldo = T > 1 ? t.ldo : M, ldmask = T > 1 ? t.ldmask : M;
+  const intptr_t out = reinterpret_cast<intptr_t>(t.out_dev), mask = reinterpret_cast<intptr_t>(t.mask_dev);
+  const __int128 between = (static_cast<__int128>(mask) - out) / size;
+  if (between >= static_cast<__int128>(T - 1) * ldo + M || -between >= static_cast<__int128>(T - 1) * ldmask + M) return true;
+  if (ldo != ldmask) return false;
+  if (between == 0) return true;
+  const int64_t column = static_cast<int64_t>((between % ldo + ldo) % ldo);       // of the mask in the result's rows
+  return column >= M && column + M <= ldo;
+}
+
 struct Call {
   int kind, variant, E;
   const int32_t* offsets;
@@ -1126,6 +1142,7 @@ mbd_status run(Call c) {
   if (!aligned16(c.A) || !aligned16(c.B) || !aligned16(t->out_dev) || !aligned16(t->mask_dev)) return MBD_E_UNSUPPORTED;
   if ((reinterpret_cast<uintptr_t>(t->bias_dev) | reinterpret_cast<uintptr_t>(c.offsets) | reinterpret_cast<uintptr_t>(c.row_scale) |
        reinterpret_cast<uintptr_t>(c.ch_scale)) & 3u) return MBD_E_UNSUPPORTED;
+  if (t->op == MBD_TAIL_MASK && t->mask_dev && c.T > 0 && !mask_apart(*t, c.T, M)) return MBD_E_INVALID;
   // each tail operation belongs to one product: bias and ReLU to the forward one, the mask to backward-data, Eq. 1 to
   // backward-weight
   if ((t->bias_dev || t->relu) && c.variant != 0) return MBD_E_UNSUPPORTED;

@@ -432,3 +432,77 @@ def test_masks_over_many_boxes_are_the_product_where_positive(kind, d_in, d_out)
     out[:T, :d_in] = mask
     mbd.expert_gemm(1, dY, W, offsets, out[:T, :d_in], op=mbd.TAIL_MASK, mask=out[:T, :d_in])
     assert torch.equal(out[:T, :d_in], want)
+
+
+@pytest.mark.parametrize("args,status", [
+    (dict(mask=(4 << 20) + 16), mbd.E_INVALID),                          # eight columns on
+    (dict(mask=(4 << 20) + 96), mbd.E_INVALID), (dict(mask=(4 << 20) - 96), mbd.E_INVALID),      # a row on, a row back
+    (dict(mask=4 << 20, ldmask=64), mbd.E_INVALID),                      # the same address, other rows
+    (dict(mask=(4 << 20) + 64 * 96 - 16), mbd.E_INVALID),                # the last eight elements
+    (dict(mask=(4 << 20) + 2 * 40, ldmask=96, ldo=96), mbd.E_INVALID),   # columns 40 .. 87 beside columns 0 .. 47
+    (dict(mask=(4 << 20) + 2 * 56, ldmask=96, ldo=96), mbd.E_INVALID),   # columns 56 .. 103: into the next row
+    (dict(T=1, mask=(4 << 20) + 16, ldmask=96), mbd.E_INVALID),
+    (dict(T=0, mask=(4 << 20) + 16), mbd.OK),
+])
+def test_a_mask_laid_over_the_result_in_another_way(args, status):
+    a = dict(variant=1, op=mbd.TAIL_MASK, ldmask=48)
+    a.update(args)
+    assert _call(**a) == status
+
+
+def test_a_mask_beside_the_result_passes_the_check():
+    # accepted calls end in the search for a device, or in a product on memory that is not there: the check alone, by what it lets through
+    # to the refusal behind it (a bias belongs to the forward product)
+    for args in (dict(mask=4 << 20), dict(mask=(4 << 20) + 64 * 96), dict(mask=(4 << 20) - 64 * 96), dict(mask=(4 << 20) + 96, ldmask=96, ldo=96),
+                 dict(mask=4 << 20, ldmask=96, ldo=96), dict(T=1, mask=(4 << 20) + 96, ldmask=480), dict(T=1, mask=4 << 20, ldmask=480)):
+        assert _call(**{**dict(variant=1, op=mbd.TAIL_MASK, ldmask=48, bias=6 << 20), **args}) == mbd.E_UNSUPPORTED
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [[0, 3, 70, 0, 33], [300, 257, 1, 0, 513]])
+@pytest.mark.parametrize("d_in", [264, 131])
+def test_masks_over_several_segments(counts, d_in):
+    """A float result whose K is more than eight pieces of 4096, so that no form keeps it in one accumulation: the mask in memory of its
+    own and in the result's.  Every element is the unmasked one or zero, bit for bit."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(d_in + sum(counts))
+    d_out, E, T, ld = 33000, len(counts), sum(counts) + 7, -(-d_in // 8) * 8
+    bounds = _bounds(counts, 2)
+    offsets = torch.from_numpy(bounds.astype(np.int32)).cuda()
+    inside = slice(2, 2 + sum(counts))
+    dY, W = _bf((T, d_out), gen), _bf((E, d_out, d_in), gen, ld=ld)
+    plain = torch.full((T, ld), 7.0, device="cuda")
+    mbd.expert_gemm(1, dY, W, offsets, plain[:, :d_in])
+    ref, mag = _reference(1, dY, W, bounds, E)
+    _check(plain[inside, :d_in], ref[inside], _slack(4096, mag[inside], ref[inside], torch.float32) + (d_out / 4096 + 1) * 2.0 ** -23 * mag[inside])
+    mask = torch.randn(T, ld, device="cuda", generator=gen)[:, :d_in]
+    mask[:, 0::7], mask[:, 1::7], mask[:, 2::7], mask[:, 3::7] = 0.0, -0.0, float("nan"), torch.finfo(torch.float32).min
+    mask[:, 4::7] = float("inf")
+    mask[4] = -1.0                                           # a row that the mask leaves empty
+    want = torch.where(mask > 0, plain[:, :d_in], torch.zeros((), device="cuda"))
+    out = torch.full((T, ld), 7.0, device="cuda")
+    mbd.expert_gemm(1, dY, W, offsets, out[:, :d_in], op=mbd.TAIL_MASK, mask=mask)
+    assert torch.equal(out[inside, :d_in], want[inside])
+    out[:, :d_in] = mask
+    mbd.expert_gemm(1, dY, W, offsets, out[:, :d_in], op=mbd.TAIL_MASK, mask=out[:, :d_in])
+    assert torch.equal(out[inside, :d_in], want[inside])
+    outside = [0, 1, *range(T - 5, T)]
+    assert torch.equal(out[outside, :d_in].nan_to_num(nan=5.0), mask[outside].nan_to_num(nan=5.0)) and (out[:, d_in:] == 7.0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [[0, 3, 70, 0, 33], [300, 257, 1, 0, 513]])
+@pytest.mark.parametrize("d_out", [264, 131])
+def test_bias_and_relu_over_several_segments(counts, d_out):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(d_out + sum(counts))
+    d_in, E, T = 33000, len(counts), sum(counts)
+    bounds = _bounds(counts)
+    X, W = _bf((T, d_in), gen), _bf((E, d_out, d_in), gen)
+    bias = torch.randn(E, d_out, device="cuda", generator=gen) * 100
+    out = _spread(torch.empty(T, d_out, device="cuda"), -(-d_out // 8) * 8)
+    mbd.expert_gemm(0, X, W, torch.from_numpy(bounds.astype(np.int32)).cuda(), out, relu=True, bias=bias)
+    ref, mag = _reference(0, X, W, bounds, E)
+    b = bias[torch.from_numpy(np.repeat(np.arange(E), counts)).cuda()].double()
+    want = ref + b
+    _check(out, want.relu(), _slack(4096, mag, want, torch.float32) + (d_in / 4096 + 2) * 2.0 ** -23 * (mag + b.abs()))
