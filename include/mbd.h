@@ -204,7 +204,8 @@ MBD_API mbd_status mbd_enable_momentum(mbd_net* net, float mu);
  * lives on the device).  weight_decay applies to the W_i, not to biases.  state_bits 32 or 8: how the moments are held.  The moments are
  * zero and the step count 0 when this call returns; calling it again resets them.  Of momentum and AdamW the one enabled last is in
  * force.  With master weights the masters are what is updated (in whichever order the two are enabled).  MBD_E_INVALID for rates outside
- * [0, 1), eps outside [1e-30, 1) or a negative decay, MBD_E_UNSUPPORTED for networks with convolutions and other state_bits. */
+ * [0, 1), eps outside [1e-30, 1) or a negative decay, MBD_E_UNSUPPORTED for networks with convolutions and other state_bits.  A call
+ * that fails for want of memory (MBD_E_ALLOC) leaves the network as it was; moments of another kind are made before the old ones go. */
 MBD_API mbd_status mbd_enable_adamw(mbd_net* net, double beta1, double beta2, double eps, float weight_decay, int state_bits);
 
 /* Copy weights (network dtype) and bias (float, may be NULL) device -> library / back. */

@@ -23,6 +23,14 @@ namespace {
 
 enum { ST_IDLE = 0, ST_FWD = 1, ST_BWD_UNFUSED = 2, ST_BWD_FUSED = 3 };
 
+// AdamW's moments of a layer's weights and bias (optional); with moments in 8 bits their scales, too.
+struct Moments {
+  void *m = nullptr, *v = nullptr, *bias_m = nullptr, *bias_v = nullptr;
+  float *ms = nullptr, *vs = nullptr, *bias_ms = nullptr, *bias_vs = nullptr;
+};
+
+struct AdamRates { double b1, b2, eps; float decay; int bits; };
+
 struct Layer {
   mbd_layer spec;
   int64_t d_in = 0, d_out = 0, nW = 0;
@@ -32,8 +40,7 @@ struct Layer {
   float* W32 = nullptr;  // fp32 master weights (optional)
   float* V = nullptr;    // momentum: velocity of W (optional), fp32
   float* Vb = nullptr;   // momentum: velocity of the bias
-  void *Am = nullptr, *Av = nullptr, *Abm = nullptr, *Abv = nullptr;             // AdamW: moments of W and of the bias (optional)
-  float *Ams = nullptr, *Avs = nullptr, *Abms = nullptr, *Abvs = nullptr;       // AdamW with moments in 8 bits: their scales
+  Moments adam;
   float* db = nullptr;
   void* act = nullptr;   // stored forward output [B, d_out]; float logits for the last FC layer
   void* dY = nullptr;    // [B, d_out] activation dtype
@@ -58,9 +65,7 @@ struct mbd_net {
   bool momentum = false;            // heavy-ball momentum: the update is a kernel of its own after the gradient
   float mu = 0.f;
   mbd_adamw* adamw = nullptr;       // AdamW: one launch over all tensors after the gradients
-  double adam_b1 = 0, adam_b2 = 0, adam_eps = 0;
-  float adam_decay = 0.f;
-  int adam_bits = 32;
+  AdamRates adam = {0, 0, 0, 0.f, 32};
   std::vector<Layer> layers;
   float* partials = nullptr;
   size_t partial_elems = 0;
@@ -256,40 +261,82 @@ mbd_status map_input(mbd_net* n) {
   return MBD_OK;
 }
 
-void free_moments(Layer& l) {
-  for (void* p : {l.Am, l.Av, l.Abm, l.Abv}) cudaFree(p);
-  for (float* p : {l.Ams, l.Avs, l.Abms, l.Abvs}) cudaFree(p);
-  l.Am = l.Av = l.Abm = l.Abv = nullptr;
-  l.Ams = l.Avs = l.Abms = l.Abvs = nullptr;
+void free_moments(Moments& a) {
+  for (void* p : {a.m, a.v, a.bias_m, a.bias_v}) cudaFree(p);
+  for (float* p : {a.ms, a.vs, a.bias_ms, a.bias_vs}) cudaFree(p);
+  a = Moments{};
 }
 
-// The network's tensors as one AdamW list: every W_i (its fp32 master if there is one) and, without decay, every bias.
-mbd_status make_adamw_list(mbd_net* n, int64_t steps) try {
+// A layer's moments, where they are not there yet, and zeros in them (on the network's stream).
+mbd_status zero_moments(mbd_net* n, const Layer& l, Moments& a, int bits) {
+  const auto zeros = [&](void** p, size_t bytes) -> mbd_status {
+    if (!*p) {
+      const mbd_status s = dev_alloc(p, bytes);
+      if (s != MBD_OK) return s;
+    }
+    CK(cudaMemsetAsync(*p, 0, bytes, n->stream));
+    return MBD_OK;
+  };
+  const size_t each = bits == 32 ? 4 : 1;
+  mbd_status s = zeros(&a.m, l.nW * each);
+  if (s == MBD_OK) s = zeros(&a.v, l.nW * each);
+  if (s == MBD_OK && l.bias) s = zeros(&a.bias_m, l.d_out * each);
+  if (s == MBD_OK && l.bias) s = zeros(&a.bias_v, l.d_out * each);
+  if (bits == 8) {
+    const size_t w = (l.nW + 255) / 256 * sizeof(float), b = (l.d_out + 255) / 256 * sizeof(float);
+    if (s == MBD_OK) s = zeros(reinterpret_cast<void**>(&a.ms), w);
+    if (s == MBD_OK) s = zeros(reinterpret_cast<void**>(&a.vs), w);
+    if (s == MBD_OK && l.bias) s = zeros(reinterpret_cast<void**>(&a.bias_ms), b);
+    if (s == MBD_OK && l.bias) s = zeros(reinterpret_cast<void**>(&a.bias_vs), b);
+  }
+  return s;
+}
+
+// The network's tensors as one AdamW list: every W_i (its fp32 master if there is one) and, without decay, every bias; moments[i] are
+// those of layer i.
+mbd_status make_adamw_list(const mbd_net* n, const std::vector<Moments>& moments, const AdamRates& r, int64_t steps, mbd_adamw** out) {
   std::vector<mbd_adamw_tensor> list;
-  for (Layer& l : n->layers) {
+  for (size_t i = 0; i < n->layers.size(); ++i) {
+    const Layer& l = n->layers[i];
+    const Moments& a = moments[i];
     mbd_adamw_tensor t{};
-    t.param_dev = l.W; t.master_dev = l.W32; t.grad_dev = l.dW; t.m_dev = l.Am; t.v_dev = l.Av; t.m_scale_dev = l.Ams; t.v_scale_dev = l.Avs;
-    t.n = l.nW; t.weight_decay = n->adam_decay; t.param_bf16 = n->dtype == MBD_BF16;
+    t.param_dev = l.W; t.master_dev = l.W32; t.grad_dev = l.dW; t.m_dev = a.m; t.v_dev = a.v; t.m_scale_dev = a.ms; t.v_scale_dev = a.vs;
+    t.n = l.nW; t.weight_decay = r.decay; t.param_bf16 = n->dtype == MBD_BF16;
     list.push_back(t);
     if (!l.bias) continue;
     t = mbd_adamw_tensor{};
-    t.param_dev = l.bias; t.grad_dev = l.db; t.m_dev = l.Abm; t.v_dev = l.Abv; t.m_scale_dev = l.Abms; t.v_scale_dev = l.Abvs; t.n = l.d_out;
+    t.param_dev = l.bias; t.grad_dev = l.db; t.m_dev = a.bias_m; t.v_dev = a.bias_v; t.m_scale_dev = a.bias_ms; t.v_scale_dev = a.bias_vs;
+    t.n = l.d_out;
     list.push_back(t);
   }
+  return mbd_adamw_create(list.data(), static_cast<int>(list.size()), r.bits, r.b1, r.b2, r.eps, steps, out);
+}
+
+// The network's list again, with the masters there are now; the moments and the step count go on.
+mbd_status remake_adamw_list(mbd_net* n) try {
+  std::vector<Moments> moments;
+  for (const Layer& l : n->layers) moments.push_back(l.adam);
+  int64_t steps = 0;
   mbd_adamw* fresh = nullptr;
-  const mbd_status s = mbd_adamw_create(list.data(), static_cast<int>(list.size()), n->adam_bits, n->adam_b1, n->adam_b2, n->adam_eps, steps, &fresh);
+  mbd_status s = mbd_adamw_get_steps(n->adamw, &steps);
+  if (s == MBD_OK) s = make_adamw_list(n, moments, n->adam, steps, &fresh);
   if (s != MBD_OK) return s;
-  if (n->adamw) mbd_adamw_destroy(n->adamw);
+  mbd_adamw_destroy(n->adamw);
   n->adamw = fresh;
   return MBD_OK;
 } catch (...) {
   return MBD_E_ALLOC;
 }
 
+// What a captured step names is about to go or to change.
+void drop_graph(mbd_net* n) {
+  if (n->graph_exec) { cudaGraphExecDestroy(n->graph_exec); n->graph_exec = nullptr; }
+}
+
 // The AdamW step over all layers from the materialised gradients, on the network's stream.
 mbd_status adamw_update(mbd_net* n, float eta) {
   double bytes = 0;
-  const double moments = n->adam_bits == 32 ? 16.0 : 4.0 + 16.0 / 256.0;
+  const double moments = n->adam.bits == 32 ? 16.0 : 4.0 + 16.0 / 256.0;
   for (const Layer& l : n->layers)
     bytes += l.nW * (moments + 4.0 + (l.W32 ? 10.0 : 2.0 * (n->dtype == MBD_BF16 ? 2.0 : 4.0))) + (l.bias ? l.d_out * (moments + 12.0) : 0.0);
   n->prof.begin(MBD_K_SGD, bytes);
@@ -303,7 +350,7 @@ void free_net(mbd_net* n) {
   if (n->adamw) mbd_adamw_destroy(n->adamw);
   for (Layer& l : n->layers) {
     cudaFree(l.W); cudaFree(l.bias); cudaFree(l.dW); cudaFree(l.db); cudaFree(l.act); cudaFree(l.dY); cudaFree(l.W32); cudaFree(l.V); cudaFree(l.Vb);
-    free_moments(l);
+    free_moments(l.adam);
   }
   cudaFree(n->partials); cudaFree(n->colsum_scratch); cudaFree(n->colsum_scratch_aux); cudaFree(n->per_sample); cudaFree(n->loss_dev);
   cudaFree(n->status); cudaFree(n->X_stage); cudaFree(n->labels_stage); cudaFree(n->X_fc); cudaFree(n->dX_fc);
@@ -569,10 +616,8 @@ extern "C" mbd_status mbd_enable_master_weights(mbd_net* n) {
     CK(widen_bf16_launch(l.W, l.W32, l.nW, n->num_sms, n->stream));
   }
   n->master = true;
-  if (n->adamw) {                    // the list names the masters from now on; moments and step count go on
-    int64_t steps = 0;
-    mbd_status s = mbd_adamw_get_steps(n->adamw, &steps);
-    if (s == MBD_OK) s = make_adamw_list(n, steps);
+  if (n->adamw) {
+    const mbd_status s = remake_adamw_list(n);
     if (s != MBD_OK) return s;
   }
   if (n->graph_exec) { cudaGraphExecDestroy(n->graph_exec); n->graph_exec = nullptr; }   // the step's launches change
@@ -605,40 +650,38 @@ extern "C" mbd_status mbd_enable_adamw(mbd_net* n, double beta1, double beta2, d
   if (!n || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 1e-30 && eps < 1.0) ||
       !(weight_decay >= 0.f && weight_decay < 1e30f)) return MBD_E_INVALID;
   if (n->conv || (state_bits != 32 && state_bits != 8)) return MBD_E_UNSUPPORTED;
-  const bool again = n->adamw && n->adam_bits == state_bits;
-  if (!again) {
-    CK(cudaStreamSynchronize(n->stream));                    // a step under way may still use the moments that go
-    if (n->adamw) { mbd_adamw_destroy(n->adamw); n->adamw = nullptr; }
-    for (Layer& l : n->layers) free_moments(l);
-  }
-  const auto zeros = [&](void** p, size_t bytes) -> mbd_status {
-    if (!*p) {
-      const mbd_status s = dev_alloc(p, bytes);
-      if (s != MBD_OK) return s;
-    }
-    CK(cudaMemsetAsync(*p, 0, bytes, n->stream));
-    return MBD_OK;
+  const AdamRates rates{beta1, beta2, eps, weight_decay, state_bits};
+  // What can fail for want of memory comes first, beside what the network has: a call that fails leaves the method, its moments and the
+  // captured step as they were.  Moments of the same kind are used again; they are zeroed once nothing can be refused any more.
+  const bool again = n->adamw && n->adam.bits == state_bits;
+  std::vector<Moments> moments;
+  mbd_adamw* list = nullptr;
+  const auto take_back = [&](mbd_status s) {
+    if (list) mbd_adamw_destroy(list);
+    if (!again)
+      for (Moments& a : moments) free_moments(a);
+    return s;
   };
-  const size_t each = state_bits == 32 ? 4 : 1;
-  for (Layer& l : n->layers) {
-    mbd_status s = zeros(&l.Am, l.nW * each);
-    if (s == MBD_OK) s = zeros(&l.Av, l.nW * each);
-    if (s == MBD_OK && l.bias) s = zeros(&l.Abm, l.d_out * each);
-    if (s == MBD_OK && l.bias) s = zeros(&l.Abv, l.d_out * each);
-    if (state_bits == 8) {
-      const size_t w = (l.nW + 255) / 256 * sizeof(float), b = (l.d_out + 255) / 256 * sizeof(float);
-      if (s == MBD_OK) s = zeros(reinterpret_cast<void**>(&l.Ams), w);
-      if (s == MBD_OK) s = zeros(reinterpret_cast<void**>(&l.Avs), w);
-      if (s == MBD_OK && l.bias) s = zeros(reinterpret_cast<void**>(&l.Abms), b);
-      if (s == MBD_OK && l.bias) s = zeros(reinterpret_cast<void**>(&l.Abvs), b);
-    }
-    if (s != MBD_OK) return s;
+  try {
+    for (const Layer& l : n->layers) moments.push_back(again ? l.adam : Moments{});
+    mbd_status s = MBD_OK;
+    for (size_t i = 0; i < moments.size() && s == MBD_OK && !again; ++i) s = zero_moments(n, n->layers[i], moments[i], state_bits);
+    if (s == MBD_OK) s = make_adamw_list(n, moments, rates, 0, &list);
+    if (s != MBD_OK) return take_back(s);
+  } catch (...) {                                            // out of host memory
+    return take_back(MBD_E_ALLOC);
   }
-  n->adam_b1 = beta1; n->adam_b2 = beta2; n->adam_eps = eps; n->adam_decay = weight_decay; n->adam_bits = state_bits;
-  const mbd_status s = make_adamw_list(n, 0);
-  if (s != MBD_OK) return s;
+  // a step under way may still use the list and the moments that go
+  if (cudaStreamSynchronize(n->stream) != cudaSuccess) { (void)cudaGetLastError(); return take_back(MBD_E_CUDA); }
+  drop_graph(n);
+  if (n->adamw) mbd_adamw_destroy(n->adamw);
+  n->adamw = list;
+  n->adam = rates;
   n->momentum = false;
-  if (n->graph_exec) { cudaGraphExecDestroy(n->graph_exec); n->graph_exec = nullptr; }   // the step's launches change
+  for (size_t i = 0; i < moments.size(); ++i) {
+    if (!again) { free_moments(n->layers[i].adam); n->layers[i].adam = moments[i]; }
+    else if (const mbd_status s = zero_moments(n, n->layers[i], n->layers[i].adam, state_bits); s != MBD_OK) return s;
+  }
   return MBD_OK;
 }
 
@@ -987,10 +1030,10 @@ extern "C" mbd_status mbd_get_tensor(mbd_net* n, int which, int layer, void* dst
       case MBD_T_MASTER: src = l.W32; size = l.nW * sizeof(float); break;
       case MBD_T_VELOCITY: src = l.V; size = l.nW * sizeof(float); break;
       case MBD_T_VELOCITY_BIAS: src = l.Vb; size = l.d_out * sizeof(float); break;
-      case MBD_T_ADAM_M: src = n->adam_bits == 32 ? l.Am : nullptr; size = l.nW * sizeof(float); break;
-      case MBD_T_ADAM_V: src = n->adam_bits == 32 ? l.Av : nullptr; size = l.nW * sizeof(float); break;
-      case MBD_T_ADAM_M_BIAS: src = n->adam_bits == 32 ? l.Abm : nullptr; size = l.d_out * sizeof(float); break;
-      case MBD_T_ADAM_V_BIAS: src = n->adam_bits == 32 ? l.Abv : nullptr; size = l.d_out * sizeof(float); break;
+      case MBD_T_ADAM_M: src = n->adam.bits == 32 ? l.adam.m : nullptr; size = l.nW * sizeof(float); break;
+      case MBD_T_ADAM_V: src = n->adam.bits == 32 ? l.adam.v : nullptr; size = l.nW * sizeof(float); break;
+      case MBD_T_ADAM_M_BIAS: src = n->adam.bits == 32 ? l.adam.bias_m : nullptr; size = l.d_out * sizeof(float); break;
+      case MBD_T_ADAM_V_BIAS: src = n->adam.bits == 32 ? l.adam.bias_v : nullptr; size = l.d_out * sizeof(float); break;
       case MBD_T_DB: src = l.db; size = l.d_out * sizeof(float); break;
       default: return MBD_E_INVALID;
     }
