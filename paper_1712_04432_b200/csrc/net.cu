@@ -292,15 +292,15 @@ mbd_status zero_moments(mbd_net* n, const Layer& l, Moments& a, int bits) {
   return s;
 }
 
-// The network's tensors as one AdamW list: every W_i (its fp32 master if there is one) and, without decay, every bias; moments[i] are
-// those of layer i.
-mbd_status make_adamw_list(const mbd_net* n, const std::vector<Moments>& moments, const AdamRates& r, int64_t steps, mbd_adamw** out) {
+// The network's tensors as one AdamW list: every W_i (its fp32 master if there is one) and, without decay, every bias; moments[i] and
+// masters[i] are those of layer i.
+mbd_status make_adamw_list(const mbd_net* n, const std::vector<Moments>& moments, const std::vector<float*>& masters, const AdamRates& r, int64_t steps, mbd_adamw** out) {
   std::vector<mbd_adamw_tensor> list;
   for (size_t i = 0; i < n->layers.size(); ++i) {
     const Layer& l = n->layers[i];
     const Moments& a = moments[i];
     mbd_adamw_tensor t{};
-    t.param_dev = l.W; t.master_dev = l.W32; t.grad_dev = l.dW; t.m_dev = a.m; t.v_dev = a.v; t.m_scale_dev = a.ms; t.v_scale_dev = a.vs;
+    t.param_dev = l.W; t.master_dev = masters[i]; t.grad_dev = l.dW; t.m_dev = a.m; t.v_dev = a.v; t.m_scale_dev = a.ms; t.v_scale_dev = a.vs;
     t.n = l.nW; t.weight_decay = r.decay; t.param_bf16 = n->dtype == MBD_BF16;
     list.push_back(t);
     if (!l.bias) continue;
@@ -312,20 +312,13 @@ mbd_status make_adamw_list(const mbd_net* n, const std::vector<Moments>& moments
   return mbd_adamw_create(list.data(), static_cast<int>(list.size()), r.bits, r.b1, r.b2, r.eps, steps, out);
 }
 
-// The network's list again, with the masters there are now; the moments and the step count go on.
-mbd_status remake_adamw_list(mbd_net* n) try {
+// The network's list again, with masters; the moments and the step count go on.
+mbd_status remake_adamw_list(const mbd_net* n, const std::vector<float*>& masters, mbd_adamw** out) {
   std::vector<Moments> moments;
   for (const Layer& l : n->layers) moments.push_back(l.adam);
   int64_t steps = 0;
-  mbd_adamw* fresh = nullptr;
-  mbd_status s = mbd_adamw_get_steps(n->adamw, &steps);
-  if (s == MBD_OK) s = make_adamw_list(n, moments, n->adam, steps, &fresh);
-  if (s != MBD_OK) return s;
-  mbd_adamw_destroy(n->adamw);
-  n->adamw = fresh;
-  return MBD_OK;
-} catch (...) {
-  return MBD_E_ALLOC;
+  const mbd_status s = mbd_adamw_get_steps(n->adamw, &steps);
+  return s != MBD_OK ? s : make_adamw_list(n, moments, masters, n->adam, steps, out);
 }
 
 // What a captured step names is about to go or to change.
@@ -606,21 +599,31 @@ extern "C" mbd_status mbd_enable_master_weights(mbd_net* n) {
   if (!n) return MBD_E_INVALID;
   if (n->dtype != MBD_BF16) return MBD_E_UNSUPPORTED;
   if (n->master) return MBD_OK;
-  if (n->conv) {
-    const mbd_status s = conv_enable_master(n->conv);
-    if (s != MBD_OK) return s;
+  // the masters, and the AdamW list that names them, beside what there is: a call that fails leaves the network as it was
+  std::vector<float*> masters;
+  mbd_adamw* list = nullptr;
+  const auto take_back = [&](mbd_status s) {
+    for (float* p : masters) cudaFree(p);
+    return s;
+  };
+  try {
+    mbd_status s = MBD_OK;
+    for (const Layer& l : n->layers) {
+      masters.push_back(nullptr);
+      s = dev_alloc(reinterpret_cast<void**>(&masters.back()), l.nW * sizeof(float));
+      if (s != MBD_OK) return take_back(s);
+      if (widen_bf16_launch(l.W, masters.back(), l.nW, n->num_sms, n->stream) != cudaSuccess) { (void)cudaGetLastError(); return take_back(MBD_E_CUDA); }
+    }
+    if (n->conv) s = conv_enable_master(n->conv);
+    if (s == MBD_OK && n->adamw) s = remake_adamw_list(n, masters, &list);     // its moments and step count go on
+    if (s != MBD_OK) return take_back(s);
+  } catch (...) {                                            // out of host memory
+    return take_back(MBD_E_ALLOC);
   }
-  for (Layer& l : n->layers) {
-    const mbd_status s = dev_alloc(reinterpret_cast<void**>(&l.W32), l.nW * sizeof(float));
-    if (s != MBD_OK) return s;
-    CK(widen_bf16_launch(l.W, l.W32, l.nW, n->num_sms, n->stream));
-  }
+  drop_graph(n);                     // the step's launches change
+  for (size_t i = 0; i < masters.size(); ++i) n->layers[i].W32 = masters[i];
+  if (list) { mbd_adamw_destroy(n->adamw); n->adamw = list; }
   n->master = true;
-  if (n->adamw) {
-    const mbd_status s = remake_adamw_list(n);
-    if (s != MBD_OK) return s;
-  }
-  if (n->graph_exec) { cudaGraphExecDestroy(n->graph_exec); n->graph_exec = nullptr; }   // the step's launches change
   return MBD_OK;
 }
 
@@ -663,10 +666,11 @@ extern "C" mbd_status mbd_enable_adamw(mbd_net* n, double beta1, double beta2, d
     return s;
   };
   try {
-    for (const Layer& l : n->layers) moments.push_back(again ? l.adam : Moments{});
+    std::vector<float*> masters;
+    for (const Layer& l : n->layers) { moments.push_back(again ? l.adam : Moments{}); masters.push_back(l.W32); }
     mbd_status s = MBD_OK;
     for (size_t i = 0; i < moments.size() && s == MBD_OK && !again; ++i) s = zero_moments(n, n->layers[i], moments[i], state_bits);
-    if (s == MBD_OK) s = make_adamw_list(n, moments, rates, 0, &list);
+    if (s == MBD_OK) s = make_adamw_list(n, moments, masters, rates, 0, &list);
     if (s != MBD_OK) return take_back(s);
   } catch (...) {                                            // out of host memory
     return take_back(MBD_E_ALLOC);

@@ -27,6 +27,7 @@ std::vector<std::function<void()>> under_way[2];
 int current = 0, fail_in = -1;
 bool late = false;
 long long violations = 0, adamw_launches = 0;
+int masters = 0;              // in the list of the last AdamW launch
 Graph* capture = nullptr;
 std::vector<Graph*> executables;
 
@@ -50,11 +51,13 @@ void launch(const AdamWLaunch& l) {
   ++adamw_launches;
   if (!live(l.tensors) || !live(l.first) || !live(l.clock) || !copies[l.dev].empty()) { ++violations; return; }
   const size_t entry = (reinterpret_cast<const char*>(l.first) - l.tensors) / l.count;
+  masters = 0;
   for (int i = 0; i < l.count; ++i)
     for (int k = 0; k < 7; ++k) {
       const void* p;
       memcpy(&p, l.tensors + i * entry + k * sizeof(void*), sizeof(p));
       if (p && !live(p)) ++violations;
+      if (p && k == 1) ++masters;
     }
   char* clock = l.clock;
   under_way[l.dev].push_back([clock] { if (live(clock)) ++*reinterpret_cast<long long*>(clock + 16); });
@@ -68,6 +71,7 @@ __attribute__((visibility("default"))) void fake_late_copies(int on) { late = on
 __attribute__((visibility("default"))) int fake_blocks() { return static_cast<int>(blocks.size()); }
 __attribute__((visibility("default"))) long long fake_violations() { return violations; }
 __attribute__((visibility("default"))) long long fake_adamw_launches() { return adamw_launches; }
+__attribute__((visibility("default"))) int fake_adamw_masters() { return masters; }
 __attribute__((visibility("default"))) void fake_set_device(int dev) { current = dev; }
 __attribute__((visibility("default"))) int fake_device() { return current; }
 

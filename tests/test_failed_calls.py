@@ -62,6 +62,11 @@ class Net:
         got = C.create_string_buffer(16 * 24 * 4)
         return self.L.mbd_get_tensor(self.h, mbd.T_ADAM_M, 0, C.addressof(got), len(got)) == mbd.OK
 
+    def masters(self):
+        """How many of the layers have a master that can be read."""
+        got = C.create_string_buffer(16 * 24 * 4)
+        return sum(self.L.mbd_get_tensor(self.h, mbd.T_MASTER, i, C.addressof(got), n * 4) == mbd.OK for i, n in enumerate((16 * 24, 24 * 8)))
+
     def close(self):
         assert self.L.mbd_net_destroy(self.h) == mbd.OK
 
@@ -101,4 +106,24 @@ def test_adamw_that_does_not_fit_after_momentum(L):
     for _ in failing(L, lambda: net.adamw(8)):
         assert net.step() == 0 and L.fake_violations() == bad and L.fake_blocks() == held
     assert net.step() == 1
+    net.close()
+
+
+@pytest.mark.parametrize("method", ["none", "adamw32", "adamw8", "momentum"])
+def test_masters_that_do_not_fit(L, method):
+    net = Net(L, mbd.BF16)
+    if method == "momentum":
+        assert L.mbd_enable_momentum(net.h, 0.9) == mbd.OK
+    if method.startswith("adamw"):
+        assert net.adamw(int(method[5:])) == mbd.OK
+    launches = int(method.startswith("adamw"))
+    named = lambda: L.fake_adamw_masters() if launches else None  # noqa: E731
+    assert net.step() == launches and net.masters() == 0 and not named()
+    held, bad = L.fake_blocks(), L.fake_violations()
+    for _ in failing(L, lambda: L.mbd_enable_master_weights(net.h)):
+        assert net.step() == launches and net.masters() == 0 and not named()
+        assert L.fake_violations() == bad and L.fake_blocks() == held
+    # now there are masters, and they are what is updated
+    assert net.masters() == 2 and L.mbd_enable_master_weights(net.h) == mbd.OK
+    assert net.step() == launches and named() in (2, None) and L.fake_violations() == bad
     net.close()
