@@ -629,23 +629,38 @@ extern "C" mbd_status mbd_enable_master_weights(mbd_net* n) {
 
 extern "C" mbd_status mbd_enable_momentum(mbd_net* n, float mu) {
   if (!n || !(mu >= 0.f && mu < 1.f)) return MBD_E_INVALID;
-  if (n->conv) {
-    const mbd_status s = conv_enable_momentum(n->conv, mu);
-    if (s != MBD_OK) return s;
+  // every layer's velocities, where they are not there yet, before any is taken over: a call that fails leaves the method as it was (and
+  // no layer with a velocity of its weights alone)
+  std::vector<float*> fresh;
+  mbd_status s = MBD_OK;
+  try {
+    fresh.assign(2 * n->layers.size(), nullptr);
+    for (size_t i = 0; i < n->layers.size() && s == MBD_OK; ++i) {
+      const Layer& l = n->layers[i];
+      if (!l.V) s = dev_alloc(reinterpret_cast<void**>(&fresh[2 * i]), l.nW * sizeof(float));
+      if (s == MBD_OK && l.bias && !l.Vb) s = dev_alloc(reinterpret_cast<void**>(&fresh[2 * i + 1]), l.d_out * sizeof(float));
+    }
+    if (s == MBD_OK && n->conv) s = conv_enable_momentum(n->conv, mu);
+  } catch (...) {                                            // out of host memory
+    s = MBD_E_ALLOC;
+  }
+  if (s != MBD_OK) {
+    for (float* p : fresh) cudaFree(p);
+    return s;
+  }
+  drop_graph(n);                     // the step's launches change
+  for (size_t i = 0; i < n->layers.size(); ++i) {
+    Layer& l = n->layers[i];
+    if (!l.V) l.V = fresh[2 * i];
+    if (!l.Vb) l.Vb = fresh[2 * i + 1];
   }
   for (Layer& l : n->layers) {
-    if (!l.V) {
-      mbd_status s = dev_alloc(reinterpret_cast<void**>(&l.V), l.nW * sizeof(float));
-      if (s == MBD_OK && l.bias) s = dev_alloc(reinterpret_cast<void**>(&l.Vb), l.d_out * sizeof(float));
-      if (s != MBD_OK) return s;
-    }
     CK(cudaMemsetAsync(l.V, 0, l.nW * sizeof(float), n->stream));
     if (l.Vb) CK(cudaMemsetAsync(l.Vb, 0, l.d_out * sizeof(float), n->stream));
   }
   n->momentum = true;
   n->mu = mu;
   if (n->adamw) { mbd_adamw_destroy(n->adamw); n->adamw = nullptr; }                     // one method at a time: the one enabled last
-  if (n->graph_exec) { cudaGraphExecDestroy(n->graph_exec); n->graph_exec = nullptr; }   // the step's launches change
   return MBD_OK;
 }
 
@@ -893,7 +908,7 @@ extern "C" mbd_status mbd_train_step(mbd_net* n, const void* X_dev, const int32_
   }
   const bool same = n->graph_exec && n->g_X == X_dev && n->g_labels == labels_dev && n->g_loss == loss_sum_dev && n->g_eta == eta;
   if (!same) {
-    if (n->graph_exec) { cudaGraphExecDestroy(n->graph_exec); n->graph_exec = nullptr; }
+    drop_graph(n);
     // first use of these buffers: build the tensor maps that refer to X outside the capture
     if (!n->mixed) n->X = X_dev;
     mbd_status s = map_input(n);

@@ -127,3 +127,19 @@ def test_masters_that_do_not_fit(L, method):
     assert net.masters() == 2 and L.mbd_enable_master_weights(net.h) == mbd.OK
     assert net.step() == launches and named() in (2, None) and L.fake_violations() == bad
     net.close()
+
+
+@pytest.mark.parametrize("before", ["none", "adamw"])
+def test_velocities_that_do_not_fit(L, before):
+    net = Net(L)
+    if before == "adamw":
+        assert net.adamw() == mbd.OK
+    launches = int(before == "adamw")
+    assert net.step() == launches
+    held, bad = L.fake_blocks(), L.fake_violations()
+    for _ in failing(L, lambda: L.mbd_enable_momentum(net.h, 0.9)):
+        assert net.step() == launches and L.fake_violations() == bad and L.fake_blocks() == held
+    # weights and biases of every layer have a velocity
+    assert net.step() == 0 and L.fake_violations() == bad
+    assert L.mbd_enable_momentum(net.h, 0.5) == mbd.OK and net.step() == 0 and L.fake_violations() == bad
+    net.close()
