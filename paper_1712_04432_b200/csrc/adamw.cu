@@ -645,7 +645,10 @@ extern "C" mbd_status mbd_adamw_set_steps(mbd_adamw* opt, int64_t steps_done) {
   c.b1_t = pow(opt->b1, static_cast<double>(steps_done));
   c.b2_t = pow(opt->b2, static_cast<double>(steps_done));
   c.t = steps_done;
-  if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(opt->clock, &c, sizeof(c), cudaMemcpyHostToDevice) != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_CUDA; }
+  // (the second wait is for the copy itself, and for those of a new list: from pageable memory it may return before it has landed, and
+  // the next step's stream need not wait for it)
+  if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(opt->clock, &c, sizeof(c), cudaMemcpyHostToDevice) != cudaSuccess ||
+      cudaDeviceSynchronize() != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_CUDA; }
   return MBD_OK;
 }
 

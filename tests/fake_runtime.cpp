@@ -68,6 +68,7 @@ void launch(const AdamWLaunch& l) {
 extern "C" {
 __attribute__((visibility("default"))) void fake_fail_in(int n) { fail_in = n; }                   // the nth allocation from now on, 0: the next
 __attribute__((visibility("default"))) void fake_late_copies(int on) { late = on != 0; }
+__attribute__((visibility("default"))) int fake_copies_under_way() { return static_cast<int>(copies[0].size() + copies[1].size()); }
 __attribute__((visibility("default"))) int fake_blocks() { return static_cast<int>(blocks.size()); }
 __attribute__((visibility("default"))) long long fake_violations() { return violations; }
 __attribute__((visibility("default"))) long long fake_adamw_launches() { return adamw_launches; }

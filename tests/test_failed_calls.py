@@ -143,3 +143,28 @@ def test_velocities_that_do_not_fit(L, before):
     assert net.step() == 0 and L.fake_violations() == bad
     assert L.mbd_enable_momentum(net.h, 0.5) == mbd.OK and net.step() == 0 and L.fake_violations() == bad
     net.close()
+
+
+def adamw_list(L, n=300, steps=0):
+    """A list of one tensor on host blocks; the buffers are kept beside the handle."""
+    buffers = [C.create_string_buffer(n * 4 + 16) for _ in range(4)]
+    at = [(C.addressof(b) + 15) // 16 * 16 for b in buffers]
+    table = (mbd.AdamWTensor * 1)(mbd.AdamWTensor(at[0], None, at[1], at[2], at[3], None, None, n, 0.0, 0, 0, 0))
+    h = C.c_void_p()
+    assert L.mbd_adamw_create(table, 1, 32, 0.9, 0.999, 1e-8, steps, C.byref(h)) == mbd.OK
+    return h, buffers
+
+
+def test_a_step_on_any_stream_may_follow_creation_and_set_steps(L):
+    # a copy from pageable host memory may return before it has landed, and only the stream it went through waits for that: what a list
+    # puts on the device has to be there when the call returns, since the step goes to a stream of the caller's
+    L.fake_late_copies(1)
+    try:
+        h, buffers = adamw_list(L, steps=5)
+        assert L.fake_copies_under_way() == 0
+        assert L.mbd_adamw_set_steps(h, 7) == mbd.OK and L.fake_copies_under_way() == 0
+        steps = C.c_int64()
+        assert L.mbd_adamw_get_steps(h, C.byref(steps)) == mbd.OK and steps.value == 7
+        assert L.mbd_adamw_destroy(h) == mbd.OK
+    finally:
+        L.fake_late_copies(0)
