@@ -500,8 +500,8 @@ MBD_API mbd_status mbd_expert_gemm_i8(int E, const int32_t* offsets_dev, int64_t
  * counts on at each replay (lr and grad_scale are captured by value).  Tensors of any length and alignment (16-byte accesses where
  * all of a tensor's bases allow it).  MBD_E_INVALID: an empty tensor, a missing pointer, a buffer that is written named twice or
  * overlapping another, rates outside [0, 1), eps outside [1e-30, 1), a negative decay, a master for float weights.  Steps of one handle
- * must not overlap each other (one stream, or ordered streams).  MBD_E_STATE: the current device is not the handle's.
- * set_steps / get_steps wait for the device. */
+ * must not overlap each other (one stream, or ordered streams).  MBD_E_STATE: the current device is not the handle's (step).
+ * set_steps / get_steps wait for the handle's device, whichever is current. */
 typedef struct mbd_adamw mbd_adamw; /* opaque */
 typedef struct {
   void* param_dev;           /* float, or bf16 if param_bf16 != 0                    */

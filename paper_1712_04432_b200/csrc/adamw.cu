@@ -527,6 +527,20 @@ cudaError_t ready(int* resident) {
   return e != cudaSuccess ? e : cudaOccupancyMaxActiveBlocksPerMultiprocessor(resident, adamw_kernel<BITS>, THREADS, smem_bytes<BITS>());
 }
 
+// The list's device as the current one, for the calls that wait for it or reach its memory; then the caller's again.
+class OnDevice {
+ public:
+  explicit OnDevice(int dev) : ok_(cudaGetDevice(&before_) == cudaSuccess && (before_ == dev || cudaSetDevice(dev) == cudaSuccess)), back_(ok_ && before_ != dev) {}
+  ~OnDevice() { if (back_) (void)cudaSetDevice(before_); }
+  OnDevice(const OnDevice&) = delete;
+  OnDevice& operator=(const OnDevice&) = delete;
+  explicit operator bool() const { return ok_; }
+
+ private:
+  int before_ = 0;
+  bool ok_, back_;
+};
+
 }  // namespace
 }  // namespace mbd
 
@@ -647,7 +661,8 @@ extern "C" mbd_status mbd_adamw_set_steps(mbd_adamw* opt, int64_t steps_done) {
   c.t = steps_done;
   // (the second wait is for the copy itself, and for those of a new list: from pageable memory it may return before it has landed, and
   // the next step's stream need not wait for it)
-  if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(opt->clock, &c, sizeof(c), cudaMemcpyHostToDevice) != cudaSuccess ||
+  const OnDevice on(opt->dev);
+  if (!on || cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(opt->clock, &c, sizeof(c), cudaMemcpyHostToDevice) != cudaSuccess ||
       cudaDeviceSynchronize() != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_CUDA; }
   return MBD_OK;
 }
@@ -655,7 +670,8 @@ extern "C" mbd_status mbd_adamw_set_steps(mbd_adamw* opt, int64_t steps_done) {
 extern "C" mbd_status mbd_adamw_get_steps(mbd_adamw* opt, int64_t* steps_done_host) {
   if (!opt || !steps_done_host) return MBD_E_INVALID;
   Clock c{};
-  if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&c, opt->clock, sizeof(c), cudaMemcpyDeviceToHost) != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_CUDA; }
+  const OnDevice on(opt->dev);
+  if (!on || cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&c, opt->clock, sizeof(c), cudaMemcpyDeviceToHost) != cudaSuccess) { (void)cudaGetLastError(); return MBD_E_CUDA; }
   *steps_done_host = c.t;
   return MBD_OK;
 }

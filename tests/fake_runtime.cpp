@@ -92,6 +92,8 @@ cudaError_t cudaFree(void* p) {
 }
 cudaError_t cudaMallocHost(void** p, size_t bytes) { *p = malloc(bytes); return cudaSuccess; }
 cudaError_t cudaFreeHost(void* p) { free(p); return cudaSuccess; }
+__attribute__((visibility("default"))) void* fake_malloc(size_t bytes) { void* p; return cudaMalloc(&p, bytes) == cudaSuccess ? p : nullptr; }
+__attribute__((visibility("default"))) void fake_free(void* p) { cudaFree(p); }
 cudaError_t cudaMemcpy(void* dst, const void* src, size_t bytes, cudaMemcpyKind kind) {
   for (const Copy& c : copies[current]) memcpy(c.dst, c.bytes.data(), c.bytes.size());              // copies of one stream come in order
   copies[current].clear();

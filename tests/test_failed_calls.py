@@ -1,6 +1,6 @@
 """The host code of a network and of an AdamW list on a CUDA runtime in host memory (fake_runtime.cpp): allocations that fail
-part of the way.  A call that fails leaves the network as it was, its captured step included: nothing that a later step
-launches or replays names memory that is gone."""
+part of the way (a call that fails leaves the network as it was, its captured step included: nothing that a later step
+launches or replays names memory that is gone), copies that land late, and two devices."""
 import ctypes as C
 import os
 import subprocess
@@ -34,6 +34,7 @@ def L(tmp_path_factory):
     lib.mbd_enable_momentum.argtypes = [vp, C.c_float]
     lib.mbd_adamw_get_steps.argtypes, lib.mbd_adamw_set_steps.argtypes = [vp, C.POINTER(i64)], [vp, i64]
     lib.fake_violations.restype = lib.fake_adamw_launches.restype = i64
+    lib.fake_malloc.restype, lib.fake_malloc.argtypes, lib.fake_free.argtypes = vp, [C.c_size_t], [vp]
     lib.fake_fail_in.argtypes, lib.fake_set_device.argtypes = [i32], [i32]
     yield lib
     assert lib.fake_blocks() == 0 and lib.fake_violations() == 0
@@ -146,13 +147,18 @@ def test_velocities_that_do_not_fit(L, before):
 
 
 def adamw_list(L, n=300, steps=0):
-    """A list of one tensor on host blocks; the buffers are kept beside the handle."""
-    buffers = [C.create_string_buffer(n * 4 + 16) for _ in range(4)]
-    at = [(C.addressof(b) + 15) // 16 * 16 for b in buffers]
+    """A list of one tensor, and its buffers."""
+    at = [L.fake_malloc(n * 4) for _ in range(4)]
     table = (mbd.AdamWTensor * 1)(mbd.AdamWTensor(at[0], None, at[1], at[2], at[3], None, None, n, 0.0, 0, 0, 0))
     h = C.c_void_p()
     assert L.mbd_adamw_create(table, 1, 32, 0.9, 0.999, 1e-8, steps, C.byref(h)) == mbd.OK
-    return h, buffers
+    return h, at
+
+
+def gone(L, h, buffers):
+    assert L.mbd_adamw_destroy(h) == mbd.OK
+    for p in buffers:
+        L.fake_free(p)
 
 
 def test_a_step_on_any_stream_may_follow_creation_and_set_steps(L):
@@ -165,6 +171,26 @@ def test_a_step_on_any_stream_may_follow_creation_and_set_steps(L):
         assert L.mbd_adamw_set_steps(h, 7) == mbd.OK and L.fake_copies_under_way() == 0
         steps = C.c_int64()
         assert L.mbd_adamw_get_steps(h, C.byref(steps)) == mbd.OK and steps.value == 7
-        assert L.mbd_adamw_destroy(h) == mbd.OK
+        gone(L, h, buffers)
     finally:
         L.fake_late_copies(0)
+
+
+def test_the_step_count_from_another_current_device(L):
+    # steps under way are waited for on the list's device, whichever is current, and that stays current
+    h, buffers = adamw_list(L)
+    steps = C.c_int64()
+    for _ in range(3):
+        assert L.mbd_adamw_step(h, 0.1, 1.0, 0x5000) == mbd.OK
+    L.fake_set_device(1)
+    try:
+        assert L.mbd_adamw_step(h, 0.1, 1.0, 0x5000) == mbd.E_STATE
+        assert L.mbd_adamw_get_steps(h, C.byref(steps)) == mbd.OK and steps.value == 3 and L.fake_device() == 1
+        L.fake_set_device(0)
+        assert L.mbd_adamw_step(h, 0.1, 1.0, 0x5000) == mbd.OK
+        L.fake_set_device(1)
+        assert L.mbd_adamw_set_steps(h, 10) == mbd.OK and L.fake_device() == 1      # after the step under way, not before it
+        assert L.mbd_adamw_get_steps(h, C.byref(steps)) == mbd.OK and steps.value == 10
+    finally:
+        L.fake_set_device(0)
+    gone(L, h, buffers)
