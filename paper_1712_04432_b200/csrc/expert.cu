@@ -1128,7 +1128,7 @@ mbd_status run(Call c) {
   if (!c.A || !c.B || !t || !t->out_dev || c.variant < 0 || c.variant > 2 || c.E < 1 || c.T < 0 || c.d_out < 1 || c.d_in < 1) return MBD_E_INVALID;
   if (t->op != MBD_TAIL_STORE && t->op != MBD_TAIL_MASK && t->op != MBD_TAIL_SGD) return MBD_E_INVALID;
   if (!c.offsets && c.E != 1) return MBD_E_INVALID;
-  if (c.kind == KIND_I8 && (!c.row_scale || !c.ch_scale)) return MBD_E_INVALID;
+  if (c.kind == KIND_I8 && ((!c.row_scale && c.T > 0) || !c.ch_scale)) return MBD_E_INVALID;
   const int unit = c.kind == KIND_I8 ? 16 : 8;                  // elements of 16 bytes
   const int64_t cols_a = c.variant == 0 ? c.d_in : c.d_out, cols_b = c.d_in;
   const int64_t M = c.variant == 0 ? c.d_out : c.d_in;          // channels of the result

@@ -268,3 +268,22 @@ def test_the_binding_refuses_what_it_would_misread():
                 dict(status=s)):
         with pytest.raises(AssertionError):
             mbd.gemm_i8(**{**dict(A=q, a_scale=s, B=B, b_scale=sb, out=out), **bad})
+
+
+def test_no_rows_is_no_work_without_a_device():
+    # row tensors of no rows may be null, their scales too; the weights' scales are there all the same
+    assert _gemm(experts=2, M=0) == mbd.OK and _gemm(experts=2, M=0, A=None, sa=None, out=None) == mbd.OK
+    assert _gemm(experts=2, M=0, sb=None) == mbd.E_INVALID and _gemm(experts=2, M=1, sa=None) == mbd.E_INVALID
+
+
+@pytest.mark.gpu
+def test_an_empty_batch_through_the_binding():
+    import torch
+    X, W = torch.randn(5, 64, device="cuda"), torch.randn(3, 24, 64, device="cuda")
+    wq, ws = torch.empty(3, 24, 64, dtype=torch.int8, device="cuda"), torch.empty(3, 24, device="cuda")
+    mbd.quantize_rows(W, wq, ws)
+    q, s = torch.empty(0, 64, dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda")
+    mbd.quantize_rows(X[:0], q, s)
+    for dt in (torch.bfloat16, torch.float32):
+        out = mbd.expert_gemm_i8(q, s, wq, ws, torch.zeros(4, dtype=torch.int32, device="cuda"), torch.empty(0, 24, dtype=dt, device="cuda"))
+        assert out.shape == (0, 24)
