@@ -467,9 +467,10 @@ MBD_API mbd_status mbd_expert_gemm_bf16(int variant, int E, const int32_t* offse
 
 /* ---- Products of 8-bit integers ----
  * mbd_quantize_rows: for every row of X [R, K] (bf16 if x_bf16 != 0, else float), scale[r] = max |X_r| / 127 in float and
- * Q[r, k] = X[r, k] / scale[r], correctly rounded to an integer (halves to even).  A row of zeros (or one whose scale underflows)
- * has scale 0 and Q = 0; a row with an infinity or a NaN has scale NaN and Q = 0.  A row is a token of a batch or an output
- * channel of a weight matrix; any alignment and any leading dimensions (16- and 8-byte accesses where they allow it).
+ * Q[r, k] = X[r, k] / scale[r], correctly rounded to an integer (halves to even; within +-127, which a denormal scale can miss).  A
+ * row of zeros (or one whose scale underflows) has scale 0 and Q = 0; a row with an infinity or a NaN has scale NaN and Q = 0.  A row is
+ * a token of a batch or an output channel of a weight matrix; any alignment and any leading dimensions (16- and 8-byte accesses where
+ * they allow it).
  * sync != 0: waits for the stream. */
 MBD_API mbd_status mbd_quantize_rows(const void* X_dev, int x_bf16, int64_t R, int64_t K, int64_t ldx, int8_t* Q_dev, int64_t ldq,
                              float* scale_dev, int sync, void* cuda_stream);

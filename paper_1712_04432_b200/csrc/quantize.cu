@@ -65,12 +65,14 @@ __device__ __forceinline__ Vec8<T> fetch(const T* row, int64_t i, int64_t K, boo
 }
 
 // The quotient, correctly rounded to an integer: a float quotient that is exactly half a step may have been rounded to it, the
-// remainder tells.
+// remainder tells.  (The scale is below 1e-30 here: the remainder is taken 2^64 times as large, all products being exact, since one of half
+// the smallest denormal number would be rounded to zero.)
 __device__ __noinline__ float divide_to_integer(float x, float s) {
+  constexpr float LARGE = 18446744073709551616.f;
   const float t = __fdiv_rn(x, s);
   float k = rintf(t);
   if (fabsf(t - k) == 0.5f) {
-    const float rest = fmaf(-t, s, x);
+    const float rest = fmaf(-t * LARGE, s, x * LARGE);
     if (rest > 0.f) k = ceilf(t);
     if (rest < 0.f) k = floorf(t);
   }

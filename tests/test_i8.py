@@ -277,6 +277,29 @@ def test_no_rows_is_no_work_without_a_device():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("K", [764, 33000])
+def test_half_steps_of_very_small_scales(K):
+    # scales with few bits (denormal numbers) and around the border of the special path: every half step and the floats next to it on both
+    # sides.  The quotient in 64 bits tells them apart: x / s is a half step or 2^-25 of it away at least
+    import torch
+    rng = np.random.default_rng(K)
+    tops = np.concatenate([rng.integers(1, 2 ** 23, 60) * 2.0 ** -149 * 127, rng.integers(1, 4000, 20) * 2.0 ** -149, [4.605892889927633e-39 * 127],
+                           127e-30 * rng.uniform(0.5, 2.0, 40), 127 * 2.0 ** -126 * rng.uniform(0.5, 2.0, 20)]).astype(np.float32)
+    X = np.zeros((len(tops), K), np.float32)
+    for row, top in zip(X, tops):
+        s = np.float64(np.float32(top) / np.float32(127))
+        half = (np.arange(-127, 127, dtype=np.float64) + 0.5) * s
+        x = half.astype(np.float32)
+        x = np.concatenate([x, np.nextafter(x, np.float32(np.inf)), np.nextafter(x, np.float32(-np.inf))])
+        row[1:len(x) + 1] = np.clip(x, -top, top)
+        row[0] = top
+    q, s = torch.empty(X.shape, dtype=torch.int8, device="cuda"), torch.empty(len(X), device="cuda")
+    mbd.quantize_rows(torch.from_numpy(X).cuda(), q, s, sync=True)
+    ws, wq = _want_rows(X)
+    assert np.array_equal(s.cpu().numpy(), ws) and np.array_equal(q.cpu().numpy(), wq)
+
+
+@pytest.mark.gpu
 def test_an_empty_batch_through_the_binding():
     import torch
     X, W = torch.randn(5, 64, device="cuda"), torch.randn(3, 24, 64, device="cuda")
