@@ -346,18 +346,18 @@ __device__ __forceinline__ void finish(const Params& p, const Unit& u, const uin
     // A mask over several segments is met by the first one, which may find it in the memory that it writes.  What the mask closes
     // is left as -0 for the segments to come: an open sum is never -0, it starts as a sum with +0 (and x + v is -0 for x = v = -0 only).
     constexpr uint32_t CLOSED = 0x80000000u;
-    float x[CNT], w[CNT];
-    const float* mask = reinterpret_cast<const float*>(p.mask) + base * p.ldmask + m;
+    const float closed = last ? 0.f : __uint_as_float(CLOSED);
+    const bool meets = masked && !again;
+    const float* src = meets ? reinterpret_cast<const float*>(p.mask) + base * p.ldmask + m : out;
+    const int64_t ld = meets ? p.ldmask : p.ldo;
+    float x[CNT];
+#pragma unroll
+    for (int j = 0; j < CNT; ++j) x[j] = here && j < rows ? src[j * ld] : 0.f;
 #pragma unroll
     for (int j = 0; j < CNT; ++j) {
-      x[j] = here && j < rows && (p.op == EPI_SGD || again) ? out[j * p.ldo] : 0.f;
-      w[j] = here && j < rows && masked && !again ? mask[j * p.ldmask] : 1.f;
-    }
-#pragma unroll
-    for (int j = 0; j < CNT; ++j) {
-      const bool open = w[j] > 0.f && !(masked && __float_as_uint(x[j]) == CLOSED);
       if (p.op == EPI_SGD) v[j] = fmaf(p.scale, v[j], x[j]);
-      else v[j] = open ? x[j] + v[j] : last ? 0.f : __uint_as_float(CLOSED);
+      else if (meets) v[j] = x[j] > 0.f ? v[j] + 0.f : closed;
+      else v[j] = masked && __float_as_uint(x[j]) == CLOSED ? closed : x[j] + v[j];
     }
   }
   if (!here) return;
