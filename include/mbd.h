@@ -446,7 +446,10 @@ MBD_API mbd_status mbd_softmax_xent(const float* logits_dev, int64_t B, int64_t 
  *   variant 1 (backward-data)    dX[r, :] = dY[r, :] W_e, masked               A = dY [T, d_out], B = W [E][d_out, d_in], out = dX [T, d_in]
  *   variant 2 (backward-weight)  dW_e     = sum over the group dY_r^T X_r      A = dY [T, d_out], B = X [T, d_in],        out = dW [E][d_out, d_in]
  * bf16 operands, fp32 accumulation; a float result is summed from segments of 4096 elements of K in full float arithmetic (the
- * tensor core truncates as it accumulates, about 1.1e-9 relative per element of K; a bf16 result is accumulated in one piece).
+ * tensor core truncates as it accumulates, about 1.1e-9 relative per element of K; a bf16 result is accumulated in one piece, which
+ * its own rounding of up to 2^-8 hides to K of a few hundred thousand: take a float result for longer sums).
+ * The launch is planned from T, not from the groups, which are known on the device only: few rows in groups of a long padded buffer
+ * run in the form for T rows, as exact but slower than on views of about their length.
  * A group may be empty and any length; variant 2 writes zeros for an empty one.  Rows of `out` outside every group (before offsets[0],
  * from offsets[E] on) are left as they are.  Offsets are clamped to [0, T] and a falling one counts as the largest before it, so
  * whatever they hold nothing outside the buffers is touched.  `out` overlaps neither A nor B.  Rows of different groups never meet in a sum: infinities or NaN in

@@ -9,7 +9,7 @@
 // computed from the new moments before they are rounded.
 //
 // Bound by HBM: 30 bytes per element with float moments, bf16 weights, float masters and gradients, 18 with 8 bits, 8 with 8 bits and
-// bf16 throughout.  58.6 M elements: 0.292 ms (6.0 TB/s, 92 % of the measured copy rate) and 0.206 ms (5.1 TB/s); 48 M elements in 240
+// bf16 throughout.  58.6 M elements: 0.292 - 0.298 ms (5.9 - 6.0 TB/s, 90 - 92 % of the measured copy rate) and 0.206 ms (5.1 TB/s); 48 M elements in 240
 // tensors, all bf16 and 8 bits: 0.103 ms (3.7 TB/s: there the instructions count, about 50 per element of them).  A warp owns 256
 // consecutive elements, so that a block's maximum is one warp reduction; a thread block takes one contiguous range of the list
 // (a stride over the whole grid was 1 % faster on a few large tensors and 28 % slower on many).

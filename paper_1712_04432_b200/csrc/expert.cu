@@ -15,9 +15,10 @@
 // One persistent CTA (or CTA pair, cta_group::2: 256 channels x up to 256 rows, each CTA loads its 128 channels and half
 // of the rows) per SM; warp roles as in the dense kernel: 0 TMA producer, 1 MMA issuer, 2..9 epilogue, and for
 // variant 2 a warp 10 that clears what the last k-block of a group holds of the next group (see `fixer`).
-// Measured (one B200, in a graph): 8 experts, 8192 rows, 4096 -> 4096 forward 0.209 ms (1.31 PFLOP/s; the dense kernel 1.5 on one
-// matrix), their weight gradients in float 0.245 ms (1.12 PFLOP/s: with both operands MN-major a k-block takes 0.43 us instead of
-// 0.33, in the dense kernel as well); 16 tokens over 64 experts of 1024 -> 4096 41 us (5.2 TB/s); int8 8192^3 0.315 ms (3.5 Pop/s).
+// Measured (one B200, in a graph): 8 experts, 8192 rows, 4096 -> 4096 forward 0.209 - 0.214 ms (1.28 - 1.31 PFLOP/s; the dense kernel 1.5 on
+// one matrix), their weight gradients in float 0.245 - 0.262 ms (1.05 - 1.12 PFLOP/s: with both operands MN-major a k-block takes 0.43 us
+// instead of 0.33, in the dense kernel as well); 16 tokens over 64 experts of 1024 -> 4096 41 us (5.2 TB/s); int8 8192^3 0.315 - 0.320 ms
+// (3.4 - 3.5 Pop/s).
 // The split form cuts K over the CTAs of a cluster and joins the pieces through distributed shared memory, for calls
 // with too few tiles to keep the SMs busy.
 // Every wait is bounded; on time-out the kernel records a code and leaves.
@@ -485,8 +486,9 @@ __device__ __forceinline__ void epilogue(const Params& p, const Groups* groups, 
     char* const out = reinterpret_cast<char*>(p.out) + (u.e * p.out_stride + (u.row0 + lr) * p.ldo + ch) * SIZE;
     const char* const mask_at = reinterpret_cast<const char*>(p.mask) + ((u.row0 + lr) * p.ldmask + ch) * SIZE;
     // A mask arrives by 16 bytes a lane straight into the boxes, zeros beyond the group, two boxes early.  5003 rows of 16 groups, 4096
-    // channels, K = 64 and 1000: 33 and 53 us (27 and 49 without a mask).  By loads into registers a box early 44 and 59 us: a latency
-    // under load of 1.8 us per box; two boxes early in twice the registers 52 and 66.  By bulk copies it queues behind the operands'.
+    // channels, K = 64 and 1000, side by side on one set of groups: 33 and 53 us (27 and 49 without a mask); by loads into registers a box
+    // early 44 and 59 us, a latency under load of 1.8 us per box; two boxes early in twice the registers 52 and 66; by bulk copies it
+    // queues behind the operands'.  Over equal and skewed groups of those sizes 35 - 37 and 57 - 60 us (27 - 29 and 52 - 58 without a mask).
     auto fetch = [&](int b, uint32_t at) {
       if (b < count) {
         const uint32_t to = smem_u32(boxes) + at * BOX_BYTES + lane * 16;
@@ -1048,9 +1050,10 @@ int64_t most_units(int variant, int E, int64_t T, int64_t M, int64_t N, int BN, 
 }
 
 // The form of a call, by a model in SM clocks: waves of tiles over the SMs (or pairs of them), a tile's k-blocks, what a tile costs
-// beside them and, for the split forms, joining the pieces.  A k-block costs four instructions of at least 100 clocks whatever their
-// number of rows (540 for a pair, measured: halving a pair's rows took 8 % off a tile's time), or filling shared memory at about 70 bytes a
-// clock.  The group sizes are not known here: rows spread evenly over the experts they can touch, a tile and a half each beyond one.
+// beside them and, for the split forms, joining the pieces.  A k-block of these kernels takes at least 400 clocks however few its rows
+// (540 for a pair: halving a pair's rows took 8 % off a tile's time; the ring has as many stages then as for the widest tile), or filling
+// shared memory at about 70 bytes a clock.  The group sizes are not known here: the T rows of the row tensors, padding included, spread evenly
+// over the experts they can touch, a tile and a half each beyond one.
 // Measured with 16 rows of K = 9216 int8 on 4096 channels: 28 us by the pair form, 12.9 us split in 4; 8192 rows: 0.31 ms by the pair
 // form, and 128-row tiles twice that.
 Launch plan(int kind, int variant, int E, int64_t T, int64_t M, int64_t N, int64_t K, bool out_f32, int sms) {

@@ -623,7 +623,7 @@ def expert_gemm(variant: int, A, B, offsets, out, op: int = TAIL_STORE, relu: bo
       variant 0: A = X [T, d_in], B = W [E, d_out, d_in], out [T, d_out], bias [E, d_out] float or None, relu
       variant 1: A = dY [T, d_out], B = W [E, d_out, d_in], out [T, d_in], op TAIL_MASK with mask [T, d_in] or None
       variant 2: A = dY [T, d_out], B = X [T, d_in], out [E, d_out, d_in], op TAIL_SGD with scale
-    bf16 operands with free row strides (multiples of 8), `out` bf16 or float; `mask` in out's type.  Rows of `out` in no group
+    bf16 operands with free row strides (multiples of 8), `out` bf16 or float; `mask` in out's type, `out` itself or apart from it.  Rows of `out` in no group
     stay as they are.  `status` (int32 CUDA tensor of one zero): enqueue only; otherwise the call waits for the stream."""
     dev, stream = _device()
     sa, sb, so = A.shape, B.shape, offsets.shape
