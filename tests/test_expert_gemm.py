@@ -506,3 +506,22 @@ def test_bias_and_relu_over_several_segments(counts, d_out):
     b = bias[torch.from_numpy(np.repeat(np.arange(E), counts)).cuda()].double()
     want = ref + b
     _check(out, want.relu(), _slack(4096, mag, want, torch.float32) + (d_in / 4096 + 2) * 2.0 ** -23 * (mag + b.abs()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("variant", [0, 1, 2])
+def test_the_most_experts_there_may_be(variant):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(variant)
+    E, d_in, d_out = 512, 72, 40
+    counts = torch.randint(0, 4, (E,), device="cuda", generator=gen).tolist()
+    counts[17], counts[511] = 300, 70
+    bounds, T = _bounds(counts, 1), sum(counts) + 3
+    X, dY, W = _bf((T, d_in), gen), _bf((T, d_out), gen), _bf((E, d_out, d_in), gen)
+    A, B = ((X, W), (dY, W), (dY, X))[variant]
+    out = torch.zeros(((T, d_out), (T, d_in), (E, d_out, d_in))[variant], device="cuda")
+    mbd.expert_gemm(variant, A, B, torch.from_numpy(bounds.astype(np.int32)).cuda(), out)
+    ref, mag = _reference(variant, A, B, bounds, E)
+    rows = slice(None) if variant == 2 else slice(1, 1 + sum(counts))
+    _check(out[rows], ref[rows], _slack(300, mag[rows], ref[rows], torch.float32))
+    assert variant == 2 or not (out[0].any() or out[-2:].any())
