@@ -458,9 +458,13 @@ def test_a_mask_beside_the_result_passes_the_check():
         assert _call(**{**dict(variant=1, op=mbd.TAIL_MASK, ldmask=48, bias=6 << 20), **args}) == mbd.E_UNSUPPORTED
 
 
+# few tiles and many (the form of 64 rows a tile, and the pairs of CTAs), sizes of whole 16 bytes and odd ones
+SEVERAL_SEGMENTS = [([0, 3, 70, 0, 33], 264), ([0, 3, 70, 0, 33], 131), ([300, 257, 1, 0, 513], 264), ([300, 257, 1, 0, 513], 131),
+                    ([700, 1, 0, 900, 390], 2056), ([700, 1, 0, 900, 390], 2055)]
+
+
 @pytest.mark.gpu
-@pytest.mark.parametrize("counts", [[0, 3, 70, 0, 33], [300, 257, 1, 0, 513]])
-@pytest.mark.parametrize("d_in", [264, 131])
+@pytest.mark.parametrize("counts,d_in", SEVERAL_SEGMENTS)
 def test_masks_over_several_segments(counts, d_in):
     """A float result whose K is more than eight pieces of 4096, so that no form keeps it in one accumulation: the mask in memory of its
     own and in the result's.  Every element is the unmasked one or zero, bit for bit."""
@@ -491,8 +495,7 @@ def test_masks_over_several_segments(counts, d_in):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("counts", [[0, 3, 70, 0, 33], [300, 257, 1, 0, 513]])
-@pytest.mark.parametrize("d_out", [264, 131])
+@pytest.mark.parametrize("counts,d_out", SEVERAL_SEGMENTS)
 def test_bias_and_relu_over_several_segments(counts, d_out):
     import torch
     gen = torch.Generator(device="cuda").manual_seed(d_out + sum(counts))
