@@ -490,6 +490,89 @@ MBD_API mbd_status mbd_expert_gemm_i8(int E, const int32_t* offsets_dev, int64_t
                               int64_t lda, const float* a_scale_dev, const int8_t* B_dev, int64_t ldb, int64_t expert_stride,
                               const float* b_scale_dev, const mbd_tail* tail, int32_t* status_dev, void* cuda_stream);
 
+/* ---- Root-mean-square norm ----
+ * Rows of K values, x bf16 (x_bf16 != 0) or float:
+ *     h = x                                    without a residual
+ *     h = x + residual, rounded to the residual's type, stored in H_dev if that is given: the residual stream moves on, and the
+ *                                              norm is of what is stored
+ *     y = h / sqrt(mean(h^2) + eps) * gain     (gain float [K], NULL: ones), rounded once to bf16 or float
+ * Y_dev receives y; Q_dev / scale_dev receive it in 8 bits, as mbd_gemm_i8 and mbd_expert_gemm_i8 read it: with u = h * gain in float, q = u / s
+ * correctly rounded to an integer where s = max |u| / 127, exactly as mbd_quantize_rows(u) has them, and scale = s / sqrt(mean(h^2) + eps)
+ * (so q does not depend on the order of the sum).  One of the two, or both.  A row with an infinity or a NaN in u has scale NaN
+ * and q = 0.  Sums in float; a row whose squares leave float's range is summed again scaled down.
+ * H_dev may be the residual's own memory, or x's if it has its type, and Y_dev the memory of x or of the residual if it has its type
+ * (same address, same leading dimension); otherwise results share no element with each other or with an input (MBD_E_INVALID).  Columns of one wider
+ * buffer are apart.  Any K, leading dimensions and alignment of whole elements (MBD_E_UNSUPPORTED otherwise); rows of 16-byte-aligned bf16
+ * and 32-byte-aligned floats with K and all leading dimensions multiples of 8 move in whole vectors.  eps in [1e-30, 1).  R = 0 is allowed.
+ * Enqueues only, keeps no state. */
+MBD_API mbd_status mbd_rms_norm(int64_t R, int64_t K, const void* X_dev, int x_bf16, int64_t ldx, const void* residual_dev, int residual_bf16,
+                        int64_t ldres, const float* gain_dev, double eps, void* H_dev, int64_t ldh, void* Y_dev, int y_bf16, int64_t ldy,
+                        int8_t* Q_dev, int64_t ldq, float* scale_dev, void* cuda_stream);
+/* Its gradients, from dY (of y) and h as the forward call stored it (x where there was no residual), r = 1 / sqrt(mean(h^2) + eps):
+ *     m = mean over the row of dY gain h r ,   dX = r (dY gain - h r m) (+ d_residual) ,   d_gain[k] = sum over the rows of dY h r
+ * d_residual_dev (may be NULL) is the gradient that arrives at h along the residual stream; h, d_residual and dX have one type
+ * (h_bf16), dX is the gradient of both x and the residual.  d_gain_dev (float [K], NULL: not asked for) is overwritten; it is summed in a
+ * fixed order through scratch_dev (min(R, MBD_NORM_SCRATCH_ROWS) * K floats, contents of no matter; calls in flight at the same time need
+ * one each).  dX_dev may be the memory of dY (same type), h or d_residual; otherwise as above. */
+enum { MBD_NORM_SCRATCH_ROWS = 592 };
+MBD_API mbd_status mbd_rms_norm_backward(int64_t R, int64_t K, const void* dY_dev, int dy_bf16, int64_t lddy, const void* H_dev, int h_bf16,
+                                 int64_t ldh, const float* gain_dev, double eps, const void* d_residual_dev, int64_t lddres, void* dX_dev,
+                                 int64_t lddx, float* d_gain_dev, float* scratch_dev, void* cuda_stream);
+
+/* ---- Routing to experts ----
+ * From the logits [T, E] (bf16 or float) of T tokens the k experts of each, their weights, and the places of the (token, slot) rows sorted by
+ * expert that the products grouped by expert want:
+ *     p = softmax(logits) or sigmoid(logits);   key = p + bias (bias_dev float [E], for balance: it has no part in the weights; NULL: none)
+ *     groups > 1: the experts are `groups` equal runs; a run's score is its largest key (group_best = 1) or the sum of its two
+ *         largest (2); the experts outside the top_groups best runs are out
+ *     ids[t, j]     the expert with the j-th largest key; equal keys by rising index (of runs, too)
+ *     weights[t, j] scale * p, or scale * p / (sum of the chosen p) with renormalise (a softmax then needs the chosen logits only)
+ *     places[t, j]  the row of slot (t, j) when all slots are sorted by expert, those of one expert by rising t;
+ *     offsets[e]    the first row of expert e, offsets[E] the number of rows: what mbd_expert_gemm_* read
+ * The choice is that of the formulas in exact arithmetic but for differences below a double's: keys that floats cannot tell apart are computed again
+ * in double.  An expert whose logit or key is -inf is never chosen; where fewer than k are left the last slots are empty: id -1, weight 0, place -1, no
+ * row.  A NaN key comes after all numbers; its weight is NaN.  count_dev (one int32 on the device, NULL: all): only the first
+ * min(max(count, 0), T) tokens are routed, the slots of the others are empty: a padded batch, in a captured graph too.
+ * ids, weights, places: dense [T, k]; offsets [E + 1].  scratch_dev: mbd_expert_route_scratch(T, E) int32 (0 for up to 64 tokens: NULL), contents
+ * of no matter; calls in flight at the same time need one each.  Results share nothing with each other or with inputs (MBD_E_INVALID).
+ * E <= 512, k <= 32, groups <= 32 (MBD_E_UNSUPPORTED beyond); k must fit into the experts of top_groups runs, E be a multiple of groups.  T = 0
+ * leaves zero offsets.  Enqueues only. */
+enum { MBD_ROUTE_SOFTMAX = 0, MBD_ROUTE_SIGMOID = 1 };
+typedef struct {
+  int32_t experts, top_k, score, renormalise;
+  int32_t groups, top_groups, group_best; /* 1, 1, 1: no groups */
+  float scale;
+} mbd_router;
+MBD_API int64_t mbd_expert_route_scratch(int64_t T, int E);
+MBD_API mbd_status mbd_expert_route(const mbd_router* router_host, int64_t T, const void* logits_dev, int logits_bf16, int64_t ld, const float* bias_dev,
+                            const int32_t* count_dev, int32_t* ids_dev, float* weights_dev, int32_t* places_dev, int32_t* offsets_dev,
+                            int32_t* scratch_dev, void* cuda_stream);
+/* The gradient of the logits from d_weights [T, k], with the choice as it is (ids outside [0, E) are empty slots; an id named twice
+ * counts twice).  d_logits [T, ldd] bf16 or float, every element written: zero where the weights do not depend on a logit. */
+MBD_API mbd_status mbd_expert_route_backward(const mbd_router* router_host, int64_t T, const void* logits_dev, int logits_bf16, int64_t ld,
+                                     const int32_t* ids_dev, const float* d_weights_dev, void* d_logits_dev, int d_logits_bf16, int64_t ldd,
+                                     void* cuda_stream);
+
+/* ---- Rows to the experts and back ----
+ * places [T, k] as mbd_expert_route leaves them, `rows` the rows of the tensor sorted by expert; a place outside [0, rows) is an empty
+ * slot.  Places are distinct (rows named twice get one of the two).  k <= 32, K any.  All enqueue only and keep no state.
+ * dispatch: out[places[t, j], :] = X[t, :], elements of 1, 2 or 4 bytes as they are, and out_scale[places[t, j]] = scale[t] for rows in 8 bits
+ *   (both NULL otherwise).  Rows of `out` in no place stay as they are.
+ * combine:  out[t, :] = residual[t, :] + sum over the slots of weights[t, j] * Y[places[t, j], :] in float in the order of j, rounded once.  weights NULL: ones
+ *   (which is dispatch's gradient); residual (out's type) NULL: zero; `out` may be the residual's own memory.  Every row of out is written.
+ * combine_backward:  dY[places[t, j], :] = weights[t, j] * d_out[t, :] (Y's type), d_weights[t, j] = sum over the columns of d_out[t, :] *
+ *   Y[places[t, j], :] (0 for an empty slot; d_weights NULL: not asked for, Y is then not read).  dY may be Y's own memory.  The gradient of the
+ *   residual is d_out itself.
+ * MBD_E_INVALID where results overlap inputs or each other in another way. */
+MBD_API mbd_status mbd_expert_dispatch(int64_t T, int k, int64_t K, int element_bytes, const void* X_dev, int64_t ldx, const float* scale_dev,
+                               const int32_t* places_dev, int64_t rows, void* out_dev, int64_t ldo, float* out_scale_dev, void* cuda_stream);
+MBD_API mbd_status mbd_expert_combine(int64_t T, int k, int64_t K, const void* Y_dev, int y_bf16, int64_t ldy, int64_t rows, const int32_t* places_dev,
+                              const float* weights_dev, const void* residual_dev, int64_t ldres, void* out_dev, int out_bf16, int64_t ldo,
+                              void* cuda_stream);
+MBD_API mbd_status mbd_expert_combine_backward(int64_t T, int k, int64_t K, const void* d_out_dev, int d_out_bf16, int64_t ldd, const void* Y_dev,
+                                       int y_bf16, int64_t ldy, int64_t rows, const int32_t* places_dev, const float* weights_dev,
+                                       void* dY_dev, int64_t lddy, float* d_weights_dev, void* cuda_stream);
+
 /* ---- AdamW over many tensors ----
  * One step over all tensors of a list in one launch, beside Eq. 1 and mbd_enable_momentum (Section 2: SGD stands for any first-order
  * method).  With g = grad * grad_scale (gradients here are sums over the batch: grad_scale = 1 / B) and t = 1, 2, .. the step:

@@ -33,7 +33,9 @@ EXPORTS = ["mbd_net_create", "mbd_net_destroy", "mbd_set_weights", "mbd_get_weig
            "mbd_conv_stage_input", "mbd_conv_forward_layer", "mbd_conv_backward_layer", "mbd_conv_outer_rows",
            "mbd_get_plan", "mbd_plan_product", "mbd_conv_forward_layer_rows", "mbd_conv_backward_layer_rows",
            "mbd_expert_gemm_bf16", "mbd_quantize_rows", "mbd_gemm_i8", "mbd_expert_gemm_i8",
-           "mbd_enable_adamw", "mbd_adamw_create", "mbd_adamw_destroy", "mbd_adamw_step", "mbd_adamw_set_steps", "mbd_adamw_get_steps"]
+           "mbd_enable_adamw", "mbd_adamw_create", "mbd_adamw_destroy", "mbd_adamw_step", "mbd_adamw_set_steps", "mbd_adamw_get_steps",
+           "mbd_rms_norm", "mbd_rms_norm_backward", "mbd_expert_route_scratch", "mbd_expert_route", "mbd_expert_route_backward",
+           "mbd_expert_dispatch", "mbd_expert_combine", "mbd_expert_combine_backward"]
 
 
 class MbdError(RuntimeError):
@@ -83,6 +85,20 @@ class Times(C.Structure):
 class GridRow(C.Structure):
     _fields_ = [("P_r", C.c_int32), ("P_c", C.c_int32), ("comm_fwd", C.c_double), ("comm_bwd", C.c_double),
                 ("comm", C.c_double), ("total", C.c_double)]
+
+
+ROUTE_SOFTMAX, ROUTE_SIGMOID = range(2)
+NORM_SCRATCH_ROWS = 592
+
+
+class Router(C.Structure):
+    """mbd_router: how tokens choose their experts (see include/mbd.h)."""
+    _fields_ = [("experts", C.c_int32), ("top_k", C.c_int32), ("score", C.c_int32), ("renormalise", C.c_int32), ("groups", C.c_int32),
+                ("top_groups", C.c_int32), ("group_best", C.c_int32), ("scale", C.c_float)]
+
+    def __init__(self, experts: int, top_k: int, score: int = ROUTE_SOFTMAX, renormalise: bool = True, groups: int = 1, top_groups: int = 1,
+                 group_best: int = 1, scale: float = 1.0):
+        super().__init__(int(experts), int(top_k), int(score), int(renormalise), int(groups), int(top_groups), int(group_best), float(scale))
 
 
 class AdamWTensor(C.Structure):
@@ -163,6 +179,14 @@ def lib():
         L.mbd_adamw_step.argtypes = [vp, f64, f64, vp]
         L.mbd_adamw_set_steps.argtypes = [vp, i64]
         L.mbd_adamw_get_steps.argtypes = [vp, C.POINTER(i64)]
+        L.mbd_rms_norm.argtypes = [i64, i64, vp, i32, i64, vp, i32, i64, vp, f64, vp, i64, vp, i32, i64, vp, i64, vp, vp]
+        L.mbd_rms_norm_backward.argtypes = [i64, i64, vp, i32, i64, vp, i32, i64, vp, f64, vp, i64, vp, i64, vp, vp, vp]
+        L.mbd_expert_route_scratch.argtypes, L.mbd_expert_route_scratch.restype = [i64, i32], i64
+        L.mbd_expert_route.argtypes = [C.POINTER(Router), i64, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.mbd_expert_route_backward.argtypes = [C.POINTER(Router), i64, vp, i32, i64, vp, vp, vp, i32, i64, vp]
+        L.mbd_expert_dispatch.argtypes = [i64, i32, i64, i32, vp, i64, vp, vp, i64, vp, i64, vp, vp]
+        L.mbd_expert_combine.argtypes = [i64, i32, i64, vp, i32, i64, i64, vp, vp, vp, i64, vp, i32, i64, vp]
+        L.mbd_expert_combine_backward.argtypes = [i64, i32, i64, vp, i32, i64, vp, i32, i64, i64, vp, vp, vp, i64, vp, vp]
         L.mbd_selftest_timeout.argtypes = [i32, vp]
         L.mbd_strerror.argtypes = [i32]
         L.mbd_strerror.restype = C.c_char_p
@@ -700,6 +724,166 @@ def expert_gemm_i8(A, a_scale, B, b_scale, offsets, out, relu: bool = False, bia
     _check(lib().mbd_expert_gemm_i8(sb[0], _at(offsets, dev), sa[0], sb[1], sb[2], _at(A, dev), lda, _at(a_scale, dev), _at(B, dev), ldb,
                                     B.stride(0), _at(b_scale, dev), C.byref(t), _word(status, dev), stream), "mbd_expert_gemm_i8")
     return out
+
+
+def _float(dtype) -> bool:
+    """Whether a tensor of bf16 or float holds bf16."""
+    assert dtype == _t.bf16 or dtype == _t.f32
+    return dtype == _t.bf16
+
+
+def _rows_at(t, shape, dev: int):
+    """(address, is bf16, row stride) of a bf16 or float tensor of `shape` [rows, K]; (None, 0, 0) for None."""
+    if t is None:
+        return None, 0, 0
+    assert t.shape == shape
+    ld, one = t.stride()
+    assert one == 1 or shape[1] == 1
+    return _at(t, dev), _float(t.dtype), (ld if shape[0] > 1 else shape[1])
+
+
+def _dense(t, dtype, shape, dev: int):
+    """Address of a contiguous tensor, or None."""
+    if t is None:
+        return None
+    assert t.dtype == dtype and t.shape == shape and t.is_contiguous()
+    return _at(t, dev)
+
+
+def rms_norm(x, gain=None, residual=None, h=None, y=None, q=None, scale=None, eps: float = 1e-6):
+    """mbd_rms_norm on rows x [R, K] (bf16 or float): y (bf16 or float) = h / sqrt(mean(h^2) + eps) * gain with h = x, or h = x + residual rounded to
+    the residual's type and stored in `h` if that is given; and / or the same in 8 bits: q (int8 [R, K]) with scale (float [R]) for
+    gemm_i8 and expert_gemm_i8.  gain: float [K] or None.  Row strides are free; `h` may be `residual` itself.  Enqueues only."""
+    dev, stream = _device()
+    shape = x.shape
+    assert len(shape) == 2
+    R, K = shape
+    ax, x_bf16, ldx = _rows_at(x, shape, dev)
+    ar, r_bf16, ldr = _rows_at(residual, shape, dev)
+    ah, h_bf16, ldh = _rows_at(h, shape, dev)
+    ay, y_bf16, ldy = _rows_at(y, shape, dev)
+    assert h is None or (residual is not None and h_bf16 == r_bf16)
+    aq, ldq, ascale = None, 0, None
+    if q is not None:
+        assert q.dtype == _t.i8 and q.shape == shape and (q.stride(1) == 1 or K == 1)
+        aq, ldq, ascale = _at(q, dev), (q.stride(0) if R > 1 else K), _dense(scale, _t.f32, (R,), dev)
+    _check(lib().mbd_rms_norm(R, K, ax, x_bf16, ldx, ar, r_bf16, ldr, _dense(gain, _t.f32, (K,), dev), eps, ah, ldh, ay, y_bf16, ldy, aq, ldq, ascale,
+                              stream), "mbd_rms_norm")
+    return y if y is not None else q
+
+
+def rms_norm_backward(dy, h, dx, gain=None, d_residual=None, d_gain=None, eps: float = 1e-6, scratch=None):
+    """mbd_rms_norm_backward: dx [R, K] (h's type) from dy (bf16 or float), h as rms_norm stored it (x without a residual) and
+    the gradient d_residual that arrives along the residual stream (h's type, or None); d_gain (float [K]) is overwritten if given.  dx may be
+    d_residual, h, or dy of its type.  scratch: float, min(R, NORM_SCRATCH_ROWS) * K, allocated here if not given.  Enqueues only."""
+    dev, stream = _device()
+    shape = h.shape
+    assert len(shape) == 2
+    R, K = shape
+    ad, d_bf16, ldd = _rows_at(dy, shape, dev)
+    ah, h_bf16, ldh = _rows_at(h, shape, dev)
+    ar, r_bf16, ldr = _rows_at(d_residual, shape, dev)
+    ax, x_bf16, ldx = _rows_at(dx, shape, dev)
+    assert x_bf16 == h_bf16 and (d_residual is None or r_bf16 == h_bf16)
+    if d_gain is not None:
+        need = min(R, NORM_SCRATCH_ROWS) * K
+        if scratch is None:
+            scratch = dx.new_empty(need, dtype=_t.f32)
+        assert scratch.dtype == _t.f32 and scratch.is_contiguous() and scratch.numel() >= need
+    _check(lib().mbd_rms_norm_backward(R, K, ad, d_bf16, ldd, ah, h_bf16, ldh, _dense(gain, _t.f32, (K,), dev), eps, ar, ldr, ax, ldx,
+                                       _dense(d_gain, _t.f32, (K,), dev), _at_or_none(scratch, dev), stream), "mbd_rms_norm_backward")
+    return dx
+
+
+def expert_route(router: Router, logits, ids, weights, places, offsets, bias=None, count=None, scratch=None):
+    """mbd_expert_route: the experts of each token.  logits [T, E] (bf16 or float) to ids (int32 [T, k]), weights (float [T, k]), places (int32 [T, k]:
+    the slots' rows sorted by expert) and offsets (int32 [E + 1], for expert_gemm).  bias: float [E], for the choice alone; count: one int32 on
+    the GPU, the tokens that are there.  scratch: int32, expert_route_scratch(T, E) of them, allocated here if not given.  Enqueues only."""
+    dev, stream = _device()
+    shape = logits.shape
+    T, E = shape
+    slots = (T, router.top_k)
+    al, l_bf16, ld = _rows_at(logits, shape, dev)
+    assert E == router.experts and (count is None or (count.dtype == _t.i32 and count.numel() == 1))
+    if T > ROUTE_ONE_BLOCK:
+        need = expert_route_scratch(T, E)
+        if scratch is None:
+            scratch = ids.new_empty(need, dtype=_t.i32)
+        assert scratch.dtype == _t.i32 and scratch.is_contiguous() and scratch.numel() >= need
+    _check(lib().mbd_expert_route(router, T, al, l_bf16, ld, _dense(bias, _t.f32, (E,), dev), _at_or_none(count, dev),
+                                  _dense(ids, _t.i32, slots, dev), _dense(weights, _t.f32, slots, dev), _dense(places, _t.i32, slots, dev),
+                                  _dense(offsets, _t.i32, (E + 1,), dev), _at_or_none(scratch, dev), stream), "mbd_expert_route")
+    return ids, weights, places, offsets
+
+
+ROUTE_ONE_BLOCK = 64           # up to so many tokens expert_route needs no scratch
+
+
+def expert_route_scratch(T: int, E: int) -> int:
+    """mbd_expert_route_scratch: int32 words of scratch that expert_route needs."""
+    return int(lib().mbd_expert_route_scratch(T, E))
+
+
+def expert_route_backward(router: Router, logits, ids, d_weights, d_logits):
+    """mbd_expert_route_backward: d_logits [T, E] (bf16 or float) from d_weights (float [T, k]) and the choice ids of expert_route.
+    Enqueues only."""
+    dev, stream = _device()
+    shape = logits.shape
+    T, E = shape
+    slots = (T, router.top_k)
+    assert E == router.experts
+    al, l_bf16, ld = _rows_at(logits, shape, dev)
+    ad, d_bf16, ldd = _rows_at(d_logits, shape, dev)
+    _check(lib().mbd_expert_route_backward(router, T, al, l_bf16, ld, _dense(ids, _t.i32, slots, dev), _dense(d_weights, _t.f32, slots, dev),
+                                           ad, d_bf16, ldd, stream), "mbd_expert_route_backward")
+    return d_logits
+
+
+def expert_dispatch(x, places, out, scale=None, out_scale=None):
+    """mbd_expert_dispatch: out[places[t, j]] = x[t] for rows x [T, K] of bf16, float or int8 (same type as out [rows, K]), and for rows in 8
+    bits out_scale[places[t, j]] = scale[t].  places int32 [T, k] as expert_route leaves them; rows in no place stay as they are.  Enqueues only."""
+    dev, stream = _device()
+    T, K = x.shape
+    rows, k, size = out.shape[0], places.shape[1], x.element_size()
+    assert x.dtype == out.dtype and size in (1, 2, 4) and out.shape[1] == K
+    (ldx, one), (ldo, one_out) = x.stride(), out.stride()
+    assert K == 1 or (one == 1 and one_out == 1)
+    _check(lib().mbd_expert_dispatch(T, k, K, size, _at(x, dev), ldx if T > 1 else K, _dense(scale, _t.f32, (T,), dev), _dense(places, _t.i32, (T, k), dev),
+                                     rows, _at(out, dev), ldo if rows > 1 else K, _dense(out_scale, _t.f32, (rows,), dev), stream), "mbd_expert_dispatch")
+    return out
+
+
+def expert_combine(y, places, out, weights=None, residual=None):
+    """mbd_expert_combine: out[t] = residual[t] + sum_j weights[t, j] y[places[t, j]] (y [rows, K] and out [T, K] bf16 or float, residual in
+    out's type or None, weights float [T, k] or None for ones, which is expert_dispatch's gradient).  `out` may be `residual`.  Enqueues only."""
+    dev, stream = _device()
+    shape = out.shape
+    T, K = shape
+    k = places.shape[1]
+    rows = y.shape[0]
+    ay, y_bf16, ldy = _rows_at(y, (rows, K), dev)
+    ar, r_bf16, ldr = _rows_at(residual, shape, dev)
+    ao, o_bf16, ldo = _rows_at(out, shape, dev)
+    assert residual is None or r_bf16 == o_bf16
+    _check(lib().mbd_expert_combine(T, k, K, ay, y_bf16, ldy, rows, _dense(places, _t.i32, (T, k), dev), _dense(weights, _t.f32, (T, k), dev),
+                                    ar, ldr, ao, o_bf16, ldo, stream), "mbd_expert_combine")
+    return out
+
+
+def expert_combine_backward(d_out, y, places, weights, dy, d_weights=None):
+    """mbd_expert_combine_backward: dy[places[t, j]] = weights[t, j] d_out[t] (y's type) and d_weights[t, j] = <d_out[t], y[places[t, j]]>.  dy may be
+    `y`; rows in no place stay as they are.  Enqueues only."""
+    dev, stream = _device()
+    T, K = d_out.shape
+    k, shape = places.shape[1], dy.shape
+    ad, d_bf16, ldd = _rows_at(d_out, d_out.shape, dev)
+    ay, y_bf16, ldy = _rows_at(y, shape, dev)
+    ag, g_bf16, ldg = _rows_at(dy, shape, dev)
+    assert shape[1] == K and (y is None or y_bf16 == g_bf16) and weights is not None and (y is not None or d_weights is None)
+    _check(lib().mbd_expert_combine_backward(T, k, K, ad, d_bf16, ldd, ay, g_bf16, ldy, shape[0], _dense(places, _t.i32, (T, k), dev),
+                                             _dense(weights, _t.f32, (T, k), dev), ag, ldg, _dense(d_weights, _t.f32, (T, k), dev), stream),
+           "mbd_expert_combine_backward")
+    return dy
 
 
 class AdamW:
