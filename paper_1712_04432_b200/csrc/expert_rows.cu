@@ -68,8 +68,8 @@ struct Combine {
   const float* weights;
   const void* res;
   void* out;
-  int64_t ldy, ldres, ldo, T, rows, K;
-  int k, n;
+  int64_t ldy, ldres, ldo, T, rows;
+  int K, k, n;
 };
 
 template <typename TY, typename TO, bool WIDE>
@@ -82,8 +82,8 @@ __global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ Co
   if (t >= p.T) return;
   const int32_t* places = p.places + t * p.k;
   const float* weights = p.weights ? p.weights + t * p.k : nullptr;
-  const int64_t vectors = (p.K + 8 * n - 1) / (8 * n);
-  for (int64_t c = 0; c < vectors; ++c) {
+  const int vectors = (p.K + 8 * n - 1) / (8 * n);
+  for (int c = 0; c < vectors; ++c) {
     float sum[8];
     Raw8<TO> res;
     res.clear();
@@ -120,8 +120,8 @@ struct CombineGrad {
   const float* weights;
   void* dy;
   float* dw;
-  int64_t ldd, ldy, lddy, T, rows, K;
-  int k, n;                    // n >= 32 threads per token, n / 32 warps; n > 32: the block has one token
+  int64_t ldd, ldy, lddy, T, rows;
+  int K, k, n;                    // n >= 32 threads per token, n / 32 warps; n > 32: the block has one token
 };
 
 constexpr int MAX_K = 32;
@@ -136,10 +136,10 @@ __global__ void __launch_bounds__(256) combine_backward_kernel(const __grid_cons
   const bool live = t < p.T;                             // (the same for a warp, and for a block that has one token)
   float dot = 0.f;                                       // lane j: this warp's part of slot j
   if (live) {
-    const int64_t vectors = (p.K + 8 * n - 1) / (8 * n);
+    const int vectors = (p.K + 8 * n - 1) / (8 * n);
     const int64_t place = lane < p.k ? p.places[t * p.k + lane] : -1;
     const float weight = lane < p.k ? p.weights[t * p.k + lane] : 0.f;
-    for (int64_t c = 0; c < vectors; ++c) {
+    for (int c = 0; c < vectors; ++c) {
       Raw8<TD> d;
       load8<WIDE>(static_cast<const TD*>(p.d_out) + t * p.ldd, l, c, n, p.K, d);
       for (int j = 0; j < p.k; ++j) {
@@ -260,7 +260,7 @@ extern "C" mbd_status mbd_expert_combine(int64_t T, int k, int64_t K, const void
   for (const Rows* t : {&y, &res, &out, &places, &weights})
     if (t->misplaced()) return MBD_E_UNSUPPORTED;
   if (!apart(out, y) || !apart(out, places) || !apart(out, weights) || !apart_or_same(out, res)) return MBD_E_INVALID;
-  const Combine p{Y_dev, places_dev, weights_dev, residual_dev, out_dev, ldy, ldres, ldo, T, rows, K, k, 0};
+  const Combine p{Y_dev, places_dev, weights_dev, residual_dev, out_dev, ldy, ldres, ldo, T, rows, static_cast<int>(K), k, 0};
   const bool wide = K % 8 == 0 && y.wide() && res.wide() && out.wide();
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   return done(y_bf16 ? (out_bf16 ? launch<bf16, bf16>(p, wide, stream) : launch<bf16, float>(p, wide, stream))
@@ -285,7 +285,7 @@ extern "C" mbd_status mbd_expert_combine_backward(int64_t T, int k, int64_t K, c
   for (const Rows* t : {&d, &places, &weights})
     if (!apart(dy, *t) || !apart(dw, *t)) return MBD_E_INVALID;
   if (!apart(dw, y) || !apart(dw, dy)) return MBD_E_INVALID;
-  const CombineGrad p{d_out_dev, Y_dev, places_dev, weights_dev, dY_dev, d_weights_dev, ldd, ldy, lddy, T, rows, K, k, 0};
+  const CombineGrad p{d_out_dev, Y_dev, places_dev, weights_dev, dY_dev, d_weights_dev, ldd, ldy, lddy, T, rows, static_cast<int>(K), k, 0};
   const bool wide = K % 8 == 0 && d.wide() && y.wide() && dy.wide();
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   return done(d_out_bf16 ? (y_bf16 ? launch<bf16, bf16>(p, wide, stream) : launch<bf16, float>(p, wide, stream))

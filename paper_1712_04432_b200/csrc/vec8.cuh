@@ -8,14 +8,18 @@
 // A column belongs to the same thread whatever the tensor's type, so that a result may take the place of what it was made from.
 #pragma once
 #include "epi.cuh"
+#include "pairs.cuh"
 
 namespace mbd {
 
 template <typename T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> {
   uint32_t w[4];
+  // unpacked anew from here on (the compiler would keep the floats beside the packed values: twice the registers)
+  __device__ __forceinline__ void repack() { asm volatile("" : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])); }
   __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0u; }
   __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16); }
+  __device__ __forceinline__ f32x2 two(int i) const { return pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u)); }
   __device__ __forceinline__ void set(const float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
@@ -23,11 +27,13 @@ template <> struct Raw8<__nv_bfloat16> {
 };
 template <> struct Raw8<float> {
   float f[8];
+  __device__ __forceinline__ void repack() {}
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = 0.f;
   }
   __device__ __forceinline__ float at(int i) const { return f[i]; }
+  __device__ __forceinline__ f32x2 two(int i) const { return pair(f[2 * i], f[2 * i + 1]); }
   __device__ __forceinline__ void set(const float* v) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = v[i];
@@ -49,65 +55,65 @@ __device__ __forceinline__ void write8(float* p, const Raw8<float>& r) {
                :: "l"(p), "f"(r.f[0]), "f"(r.f[1]), "f"(r.f[2]), "f"(r.f[3]), "f"(r.f[4]), "f"(r.f[5]), "f"(r.f[6]), "f"(r.f[7]) : "memory");
 }
 
-// Column of value i of vector j of thread t.
-template <bool WIDE> __device__ __forceinline__ int64_t column(int64_t t, int64_t j, int n, int i) {
+// Column of value i of vector j of thread t (rows are a little shorter than 2^31).
+template <bool WIDE> __device__ __forceinline__ int column(int t, int j, int n, int i) {
   return WIDE ? 8 * (t + j * n) + i : t + (8 * j + i) * n;
 }
 
 // Columns from K on read as zero.
 template <bool WIDE>
-__device__ __forceinline__ void load8(const __nv_bfloat16* row, int t, int64_t j, int n, int64_t K, Raw8<__nv_bfloat16>& r) {
+__device__ __forceinline__ void load8(const __nv_bfloat16* row, int t, int j, int n, int K, Raw8<__nv_bfloat16>& r) {
   r.clear();
   if (WIDE) {
     if (column<true>(t, j, n, 0) < K) read8(row + column<true>(t, j, n, 0), r);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int64_t c = column<false>(t, j, n, i);
+      const int c = column<false>(t, j, n, i);
       if (c < K) r.w[i >> 1] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[c]) << (i & 1 ? 16 : 0);
     }
   }
 }
 template <bool WIDE>
-__device__ __forceinline__ void load8(const float* row, int t, int64_t j, int n, int64_t K, Raw8<float>& r) {
+__device__ __forceinline__ void load8(const float* row, int t, int j, int n, int K, Raw8<float>& r) {
   r.clear();
   if (WIDE) {
     if (column<true>(t, j, n, 0) < K) read8(row + column<true>(t, j, n, 0), r);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int64_t c = column<false>(t, j, n, i);
+      const int c = column<false>(t, j, n, i);
       if (c < K) r.f[i] = row[c];
     }
   }
 }
 template <bool WIDE>
-__device__ __forceinline__ void store8(__nv_bfloat16* row, int t, int64_t j, int n, int64_t K, const Raw8<__nv_bfloat16>& r) {
+__device__ __forceinline__ void store8(__nv_bfloat16* row, int t, int j, int n, int K, const Raw8<__nv_bfloat16>& r) {
   if (WIDE) {
     if (column<true>(t, j, n, 0) < K) write8(row + column<true>(t, j, n, 0), r);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int64_t c = column<false>(t, j, n, i);
+      const int c = column<false>(t, j, n, i);
       if (c < K) reinterpret_cast<uint16_t*>(row)[c] = static_cast<uint16_t>(r.w[i >> 1] >> (i & 1 ? 16 : 0));
     }
   }
 }
 template <bool WIDE>
-__device__ __forceinline__ void store8(float* row, int t, int64_t j, int n, int64_t K, const Raw8<float>& r) {
+__device__ __forceinline__ void store8(float* row, int t, int j, int n, int K, const Raw8<float>& r) {
   if (WIDE) {
     if (column<true>(t, j, n, 0) < K) write8(row + column<true>(t, j, n, 0), r);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int64_t c = column<false>(t, j, n, i);
+      const int c = column<false>(t, j, n, i);
       if (c < K) row[c] = r.f[i];
     }
   }
 }
 // Floats to a row of either type.
 template <bool WIDE>
-__device__ __forceinline__ void store8(void* base, int bf16, int64_t row_start, int t, int64_t j, int n, int64_t K, const float* v) {
+__device__ __forceinline__ void store8(void* base, int bf16, int64_t row_start, int t, int j, int n, int K, const float* v) {
   if (bf16) {
     Raw8<__nv_bfloat16> r;
     r.set(v);
