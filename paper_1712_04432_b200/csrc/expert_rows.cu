@@ -62,6 +62,9 @@ __global__ void __launch_bounds__(256) dispatch_kernel(const __grid_constant__ D
     }
 }
 
+constexpr int MAX_K = 32;
+constexpr int NARROW = 128;    // threads a token where rows move element by element: offsets between a thread's columns are constants then
+
 struct Combine {
   const void* y;
   const int32_t* places;
@@ -72,44 +75,131 @@ struct Combine {
   int K, k, n;
 };
 
-template <typename TY, typename TO, bool WIDE>
-__global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ Combine p) {
-  constexpr int AT_ONCE = 4;
+// NV vectors of a thread and two slots are on their way together: the row of places, then 3 NV loads, then the sums.
+template <typename TY, typename TO, int NV, bool WIDE>
+__global__ void __launch_bounds__(512) combine_kernel(const __grid_constant__ Combine p) {
+  pdl_trigger();
+  pdl_wait();
+  const int n = WIDE ? p.n : NARROW, l = threadIdx.x & (n - 1);
+  const int64_t t = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) / n;
+  if (t >= p.T) return;
+  const int32_t* places = p.places + t * p.k;
+  const float* weights = p.weights ? p.weights + t * p.k : nullptr;
+  const TO* res_row = p.res ? static_cast<const TO*>(p.res) + t * p.ldres : nullptr;
+  TO* out_row = static_cast<TO*>(p.out) + t * p.ldo;
+  const int vectors = (p.K + 8 * n - 1) / (8 * n);
+  for (int c = 0; c < vectors; c += NV) {
+    f32x2 sum[NV][4];
+    Raw8<TO> res[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      res[v].clear();
+      if (res_row) load8<WIDE>(res_row, l, c + v, n, p.K, res[v]);
+    }
+    for (int j = 0; j < p.k; j += 2) {
+      const int64_t a = places[j], b = j + 1 < p.k ? places[j + 1] : -1;
+      const bool there_a = a >= 0 && a < p.rows, there_b = b >= 0 && b < p.rows;
+      const float wa = there_a && weights ? weights[j] : 1.f, wb = there_b && weights ? weights[j + 1] : 1.f;
+      Raw8<TY> ya[NV], yb[NV];
+      if (there_a) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) load8<WIDE>(static_cast<const TY*>(p.y) + a * p.ldy, l, c + v, n, p.K, ya[v]);
+      }
+      if (there_b) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) load8<WIDE>(static_cast<const TY*>(p.y) + b * p.ldy, l, c + v, n, p.K, yb[v]);
+      }
+      if (j == 0) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[v][i] = res[v].two(i);
+      }
+      if (there_a) {                                       // (an empty slot adds nothing, whatever its weight)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[v][i] = fma2(pair(wa, wa), ya[v].two(i), sum[v][i]);
+      }
+      if (there_b) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[v][i] = fma2(pair(wb, wb), yb[v].two(i), sum[v][i]);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 s = floats(sum[v][i]);
+        f[2 * i] = s.x;
+        f[2 * i + 1] = s.y;
+      }
+      Raw8<TO> o;
+      o.set(f);
+      store8<WIDE>(out_row, l, c + v, n, p.K, o);
+    }
+  }
+}
+
+// Up to SLOTS slots in whole vectors, all of a thread's loads under way at once and no sums held between them (8192 tokens of two
+// slots, 4096 bf16 columns: 42 us, by the kernel above 51).
+template <typename TY, typename TO, int NV, int SLOTS>
+__global__ void __launch_bounds__(512) combine_slots_kernel(const __grid_constant__ Combine p) {
   pdl_trigger();
   pdl_wait();
   const int n = p.n, l = threadIdx.x & (n - 1);
   const int64_t t = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) / n;
   if (t >= p.T) return;
-  const int32_t* places = p.places + t * p.k;
-  const float* weights = p.weights ? p.weights + t * p.k : nullptr;
+  const TO* res_row = p.res ? static_cast<const TO*>(p.res) + t * p.ldres : nullptr;
+  TO* out_row = static_cast<TO*>(p.out) + t * p.ldo;
+  const TY* row[SLOTS];
+  float w[SLOTS];
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j) {
+    const int64_t at = j < p.k ? p.places[t * p.k + j] : -1;
+    row[j] = at >= 0 && at < p.rows ? static_cast<const TY*>(p.y) + at * p.ldy : nullptr;
+    w[j] = row[j] && p.weights ? p.weights[t * p.k + j] : 1.f;
+  }
   const int vectors = (p.K + 8 * n - 1) / (8 * n);
-  for (int c = 0; c < vectors; ++c) {
-    float sum[8];
-    Raw8<TO> res;
-    res.clear();
-    if (p.res) load8<WIDE>(static_cast<const TO*>(p.res) + t * p.ldres, l, c, n, p.K, res);
+  for (int c = 0; c < vectors; c += NV) {
+    Raw8<TO> res[NV];
+    Raw8<TY> y[SLOTS][NV];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] = res.at(i);
-    for (int j0 = 0; j0 < p.k; j0 += AT_ONCE) {
-      Raw8<TY> y[AT_ONCE];
-      float w[AT_ONCE];
-      bool there[AT_ONCE];
+    for (int v = 0; v < NV; ++v) {
+      res[v].clear();
+      if (res_row) load8<true>(res_row, l, c + v, n, p.K, res[v]);
+    }
 #pragma unroll
-      for (int j = 0; j < AT_ONCE; ++j) {
-        const int64_t at = j0 + j < p.k ? places[j0 + j] : -1;
-        there[j] = at >= 0 && at < p.rows;
-        w[j] = there[j] && weights ? weights[j0 + j] : 1.f;
-        if (there[j]) load8<WIDE>(static_cast<const TY*>(p.y) + at * p.ldy, l, c, n, p.K, y[j]);
+    for (int j = 0; j < SLOTS; ++j)
+      if (row[j]) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) load8<true>(row[j], l, c + v, n, p.K, y[j][v]);
       }
 #pragma unroll
-      for (int j = 0; j < AT_ONCE; ++j)
-        if (there[j])                                    // an empty slot adds nothing, whatever its weight
+    for (int v = 0; v < NV; ++v) {
+      f32x2 sum[4];
+      float f[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[j], y[j].at(i), sum[i]);
+      for (int i = 0; i < 4; ++i) sum[i] = res[v].two(i);
+#pragma unroll
+      for (int j = 0; j < SLOTS; ++j)
+        if (row[j]) {                                      // (an empty slot adds nothing, whatever its weight)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] = fma2(pair(w[j], w[j]), y[j][v].two(i), sum[i]);
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 s = floats(sum[i]);
+        f[2 * i] = s.x;
+        f[2 * i + 1] = s.y;
+      }
+      Raw8<TO> o;
+      o.set(f);
+      store8<true>(out_row, l, c + v, n, p.K, o);
     }
-    Raw8<TO> o;
-    o.set(sum);
-    store8<WIDE>(static_cast<TO*>(p.out) + t * p.ldo, l, c, n, p.K, o);
   }
 }
 
@@ -124,46 +214,83 @@ struct CombineGrad {
   int K, k, n;                    // n >= 32 threads per token, n / 32 warps; n > 32: the block has one token
 };
 
-constexpr int MAX_K = 32;
-
-template <typename TD, typename TY, bool WIDE>
-__global__ void __launch_bounds__(256) combine_backward_kernel(const __grid_constant__ CombineGrad p) {
-  __shared__ float dots[8][MAX_K];
+// The rows of SLOTS slots are on their way together; each thread adds up its part of their dot products over the whole row, the threads meet
+// once per SLOTS slots.  (Four at a time took as long: 5003 tokens of four slots, 1000 columns, 18 us.)
+template <typename TD, typename TY, int NV, bool WIDE>
+__global__ void __launch_bounds__(512) combine_backward_kernel(const __grid_constant__ CombineGrad p) {
+  constexpr int SLOTS = 2;
+  __shared__ float dots[16][MAX_K];
   pdl_trigger();
   pdl_wait();
-  const int n = p.n, l = threadIdx.x & (n - 1), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n = WIDE ? p.n : NARROW, l = threadIdx.x & (n - 1), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t t = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) / n;
-  const bool live = t < p.T;                             // (the same for a warp, and for a block that has one token)
+  if (t >= p.T) return;                                  // (the same for a warp, and for a block that has one token)
+  const TD* d_row = static_cast<const TD*>(p.d_out) + t * p.ldd;
+  const int vectors = (p.K + 8 * n - 1) / (8 * n);
+  const int64_t place = lane < p.k ? p.places[t * p.k + lane] : -1;
+  const float weight = lane < p.k ? p.weights[t * p.k + lane] : 0.f;
   float dot = 0.f;                                       // lane j: this warp's part of slot j
-  if (live) {
-    const int vectors = (p.K + 8 * n - 1) / (8 * n);
-    const int64_t place = lane < p.k ? p.places[t * p.k + lane] : -1;
-    const float weight = lane < p.k ? p.weights[t * p.k + lane] : 0.f;
-    for (int c = 0; c < vectors; ++c) {
-      Raw8<TD> d;
-      load8<WIDE>(static_cast<const TD*>(p.d_out) + t * p.ldd, l, c, n, p.K, d);
-      for (int j = 0; j < p.k; ++j) {
-        const int64_t at = __shfl_sync(0xffffffffu, place, j);
-        if (at < 0 || at >= p.rows) continue;
-        const float w = __shfl_sync(0xffffffffu, weight, j);
-        Raw8<TY> y, o;
-        float v[8], s = 0.f;
-        if (p.dw) {
-          load8<WIDE>(static_cast<const TY*>(p.y) + at * p.ldy, l, c, n, p.K, y);
+  Raw8<TD> d[NV];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s = fmaf(d.at(i), y.at(i), s);
+  for (int v = 0; v < NV; ++v) load8<WIDE>(d_row, l, v, n, p.K, d[v]);
+  for (int j0 = 0; j0 < p.k; j0 += SLOTS) {
+    int64_t at[SLOTS];
+    float w[SLOTS];
+    bool there[SLOTS];
+    f32x2 s[SLOTS];
 #pragma unroll
-          for (int m = 16; m > 0; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
-          if (lane == j) dot += s;
+    for (int j = 0; j < SLOTS; ++j) {
+      at[j] = __shfl_sync(0xffffffffu, place, (j0 + j) & 31);
+      w[j] = __shfl_sync(0xffffffffu, weight, (j0 + j) & 31);
+      there[j] = j0 + j < p.k && at[j] >= 0 && at[j] < p.rows;
+      s[j] = pair(0.f, 0.f);
+    }
+    for (int c = 0; c < vectors; c += NV) {
+      if (vectors > NV) {                                // a row longer than the registers: read again for each group of slots
+#pragma unroll
+        for (int v = 0; v < NV; ++v) load8<WIDE>(d_row, l, c + v, n, p.K, d[v]);
+      }
+      Raw8<TY> y[SLOTS][NV];
+      if (p.dw) {
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j)
+          if (there[j]) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) load8<WIDE>(static_cast<const TY*>(p.y) + at[j] * p.ldy, l, c + v, n, p.K, y[j][v]);
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < SLOTS; ++j)
+        if (there[j]) {
+          TY* to = static_cast<TY*>(p.dy) + at[j] * p.lddy;
+#pragma unroll
+          for (int v = 0; v < NV; ++v) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 o = floats(mul2(pair(w[j], w[j]), d[v].two(i)));
+              f[2 * i] = o.x;
+              f[2 * i + 1] = o.y;
+              if (p.dw) s[j] = fma2(d[v].two(i), y[j][v].two(i), s[j]);
+            }
+            Raw8<TY> o;
+            o.set(f);
+            store8<WIDE>(to, l, c + v, n, p.K, o);
+          }
         }
+    }
+    if (p.dw) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = w * d.at(i);
-        o.set(v);
-        store8<WIDE>(static_cast<TY*>(p.dy) + at * p.lddy, l, c, n, p.K, o);
+      for (int j = 0; j < SLOTS; ++j) {
+        const float2 f = floats(s[j]);
+        float total = f.x + f.y;
+#pragma unroll
+        for (int m = 16; m > 0; m >>= 1) total += __shfl_xor_sync(0xffffffffu, total, m);
+        if (lane == j0 + j) dot = total;
       }
     }
   }
-  if (!p.dw || !live) return;
+  if (!p.dw) return;
   if (n > 32) {
     dots[warp][lane] = dot;
     __syncthreads();
@@ -188,19 +315,43 @@ template <typename V> cudaError_t launch(Dispatch p, cudaStream_t stream) {
   return launch_pdl(dispatch_kernel<V>, dim3(static_cast<unsigned>(grid)), dim3(threads), 0, stream, 1, p);
 }
 
+// Vectors of a thread: few tokens have one, for the latency; many have so many that about 200 bytes of a thread are on their way, but 32
+// threads have something to do.
+constexpr int64_t FEW = 512;
+int vectors_for(int64_t T, int64_t K, int bytes) {
+  if (T < FEW || K < 512) return 1;
+  return bytes == 2 && K >= 1024 ? 4 : 2;
+}
+
 template <typename TY, typename TO> cudaError_t launch(Combine p, bool wide, cudaStream_t stream) {
-  p.n = threads_for((p.K + 7) / 8, 256);
+  constexpr int MORE = sizeof(TY) == 2 ? 4 : 2;
+  int nv = vectors_for(p.T, p.K, sizeof(TY));
+  if (p.k > 2 && nv == 4) nv = 2;
+  p.n = wide ? threads_for((p.K + 8 * nv - 1) / (8 * nv), nv == 1 ? 512 : 256) : NARROW;
   const int threads = p.n < 128 ? 128 : p.n;
   const dim3 grid(static_cast<unsigned>((p.T * p.n + threads - 1) / threads)), block(threads);
-  return wide ? launch_pdl(combine_kernel<TY, TO, true>, grid, block, 0, stream, 1, p) : launch_pdl(combine_kernel<TY, TO, false>, grid, block, 0, stream, 1, p);
+  if (!wide) return launch_pdl(combine_kernel<TY, TO, 1, false>, grid, block, 0, stream, 1, p);
+  if (p.k <= 2) {
+    if (nv == 1) return launch_pdl(combine_slots_kernel<TY, TO, 1, 2>, grid, block, 0, stream, 1, p);
+    if (nv == 2) return launch_pdl(combine_slots_kernel<TY, TO, 2, 2>, grid, block, 0, stream, 1, p);
+    return launch_pdl(combine_slots_kernel<TY, TO, MORE, 2>, grid, block, 0, stream, 1, p);
+  }
+  if (p.k <= 4) {
+    if (nv == 1) return launch_pdl(combine_slots_kernel<TY, TO, 1, 4>, grid, block, 0, stream, 1, p);
+    return launch_pdl(combine_slots_kernel<TY, TO, MORE / 2, 4>, grid, block, 0, stream, 1, p);
+  }
+  if (nv == 1) return launch_pdl(combine_kernel<TY, TO, 1, true>, grid, block, 0, stream, 1, p);
+  return launch_pdl(combine_kernel<TY, TO, 2, true>, grid, block, 0, stream, 1, p);
 }
 
 template <typename TD, typename TY> cudaError_t launch(CombineGrad p, bool wide, cudaStream_t stream) {
-  p.n = threads_for((p.K + 7) / 8, 256);
+  const int nv = vectors_for(p.T, p.K, 4);               // (two already: results leave as fast as rows come)
+  p.n = wide ? threads_for((p.K + 8 * nv - 1) / (8 * nv), nv == 1 ? 512 : 256) : NARROW;
   const int threads = p.n == 32 ? 128 : p.n;
   const dim3 grid(static_cast<unsigned>((p.T * p.n + threads - 1) / threads)), block(threads);
-  return wide ? launch_pdl(combine_backward_kernel<TD, TY, true>, grid, block, 0, stream, 1, p)
-              : launch_pdl(combine_backward_kernel<TD, TY, false>, grid, block, 0, stream, 1, p);
+  if (!wide) return launch_pdl(combine_backward_kernel<TD, TY, 1, false>, grid, block, 0, stream, 1, p);
+  if (nv == 1) return launch_pdl(combine_backward_kernel<TD, TY, 1, true>, grid, block, 0, stream, 1, p);
+  return launch_pdl(combine_backward_kernel<TD, TY, 2, true>, grid, block, 0, stream, 1, p);
 }
 
 mbd_status done(cudaError_t e) {
