@@ -533,7 +533,7 @@ MBD_API mbd_status mbd_rms_norm_backward(int64_t R, int64_t K, const void* dY_de
  * in double.  An expert whose logit or key is -inf is never chosen; where fewer than k are left the last slots are empty: id -1, weight 0, place -1, no
  * row.  A NaN key comes after all numbers; its weight is NaN.  count_dev (one int32 on the device, NULL: all): only the first
  * min(max(count, 0), T) tokens are routed, the slots of the others are empty: a padded batch, in a captured graph too.
- * ids, weights, places: dense [T, k]; offsets [E + 1].  scratch_dev: mbd_expert_route_scratch(T, E) int32 (0 for up to 64 tokens: NULL), contents
+ * ids, weights, places: dense [T, k]; offsets [E + 1].  scratch_dev: mbd_expert_route_scratch(T, E) int32, 16-byte aligned (0 for up to 64 tokens: NULL), contents
  * of no matter; calls in flight at the same time need one each.  Results share nothing with each other or with inputs (MBD_E_INVALID).
  * E <= 512, k <= 32, groups <= 32 (MBD_E_UNSUPPORTED beyond); k must fit into the experts of top_groups runs, E be a multiple of groups.  T = 0
  * leaves zero offsets.  Enqueues only. */

@@ -1,14 +1,18 @@
 // Routing of tokens to experts: from a token's scores of E experts the k best ones, their weights, and the places of the (token, slot)
 // rows in the order of the experts that the products grouped by expert want; and the gradient of the logits.
 //
-//   p = softmax(l) or sigmoid(l);  key = p + bias, or the logit itself without a bias (the same order, and exact)
+//   p = softmax(l) or sigmoid(l);  key = p + bias, or the logit itself without a bias (the same order)
 //   an expert whose logit or key is -inf is never chosen;  NaN keys come after all numbers
 //   groups: a group's score is its best key, or the sum of its two best (without a bias: of its two best p);  only the best groups stay
 //   the k largest keys, equal ones by rising index;  w = c p, or c p / (sum of the chosen p)
 //
-// One warp per token, its keys in registers as integers in the order of the floats: a maximum is one warp-wide instruction.  Keys
-// made of float scores can lie nearer to each other than they are exact; where a choice hangs on such a gap the warp takes the
-// token again in double (about one token in a thousand with a bias).
+// One warp per token, a lane having NPL experts in a row.  Keys are integers, their lowest bits (one to four) giving way to the expert's
+// place in the lane: a lane sorts its keys once by minima and maxima, and each choice is one warp-wide maximum, the first lane that has
+// it, and that lane's list moving up.  Logits become integers of the same order.  Scores plus biases are counted in steps of 2^-30: a score next
+// to one is known by what it lacks, which a float has to 4e-7 of itself, so that keys of the best experts are good to some 1e-8, where their
+// sum as a float would be good to 1e-7.  What that cannot tell apart (unless logits and biases are the same) is settled in
+// double, about one token in ten thousand: it costs a token's warp, and so the whole call, microseconds.  (With keys as floats one token in 300
+// was: 8150 tokens of 256 experts 29 us.)
 //
 // Places: a block marks for each expert which of 64 tokens chose it, one bit a token, so a slot's rank is a count of bits and neither
 // it nor anything else depends on the order of atomics.  A second kernel adds up the blocks' counts (up to 64 tokens are one block, and one launch).
@@ -23,7 +27,7 @@ namespace {
 typedef __nv_bfloat16 bf16;
 constexpr int MAX_E = 512, MAX_K = 32, MAX_G = 32;
 constexpr int SUB = 64;                        // tokens whose choices are held as bits at a time
-constexpr int MOST_BLOCKS = 256, MOST_TOKENS = 65472;   // of the first kernel; of one of its blocks (counts are 16 bits wide)
+constexpr int MOST_BLOCKS = 148, MOST_TOKENS = 65472;   // of the first kernel; of one of its blocks (counts are 16 bits wide)
 
 struct Route {
   const void* logits;
@@ -31,42 +35,36 @@ struct Route {
   const int32_t* count;
   int32_t *ids, *places, *offsets;
   float* weights;
-  uint16_t* counts;             // [blocks][E2]: slots of a block's tokens per expert; null: one block does it all
+  uint16_t* counts;             // [blocks][E8]: slots of a block's tokens per expert; null: one block does it all
   int64_t ld;
-  int T, E, E2, k, chunk;       // E2: E rounded up to an even number
+  int T, E, E8, k, chunk;       // E8: E rounded up to a multiple of 8
+  int whole;                    // rows of logits can be read in whole runs of a lane's experts
   int sigmoid, renorm, G, top_groups, best;
   uint32_t by_group;            // e / (E / G) = e * by_group >> 20
+  int group_lanes;              // where every lane has experts of one group: 1 + log2 of the lanes of a group; else 0
   float scale;
 };
 
-// ---- numbers as integers of the same order; 0: not there, 1: NaN
-template <typename F> struct Code;
-template <> struct Code<float> {
-  typedef uint32_t type;
-  static __device__ __forceinline__ uint32_t of(float f) {
-    const uint32_t u = __float_as_uint(f + 0.f);               // (-0 is 0)
-    return f != f ? 1u : u & 0x80000000u ? ~u : u | 0x80000000u;
-  }
-  static __device__ __forceinline__ float value(uint32_t c) { return c <= 1u ? CUDART_NAN_F : __uint_as_float(c & 0x80000000u ? c & 0x7FFFFFFFu : ~c); }
-  static __device__ __forceinline__ uint32_t largest(uint32_t c) { return __reduce_max_sync(0xffffffffu, c); }
-  static __device__ __forceinline__ float exponential(float x) { return expf(x); }
-};
-template <> struct Code<double> {
-  typedef unsigned long long type;
-  static __device__ __forceinline__ type of(double f) {
-    const type u = static_cast<type>(__double_as_longlong(f + 0.0));
-    return f != f ? 1ull : u >> 63 ? ~u : u | 0x8000000000000000ull;
-  }
-  static __device__ __forceinline__ double value(type c) {
-    return c <= 1ull ? CUDART_NAN : __longlong_as_double(static_cast<long long>(c >> 63 ? c & 0x7FFFFFFFFFFFFFFFull : ~c));
-  }
-  static __device__ __forceinline__ type largest(type c) {
-    const uint32_t hi = static_cast<uint32_t>(c >> 32), top = __reduce_max_sync(0xffffffffu, hi);
-    const uint32_t low = __reduce_max_sync(0xffffffffu, hi == top ? static_cast<uint32_t>(c) : 0u);
-    return static_cast<type>(top) << 32 | low;
-  }
-  static __device__ __forceinline__ double exponential(double x) { return exp(x); }
-};
+// ---- numbers as integers of the same order; 0: not there, NAN_CODE: NaN (below all numbers, with room for the low bits)
+constexpr uint32_t NAN_CODE = 16;
+__device__ __forceinline__ uint32_t code_of(float f) {
+  const uint32_t u = __float_as_uint(f + 0.f);                 // (-0 is 0)
+  return f != f ? NAN_CODE : u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t c) { return c <= 2 * NAN_CODE ? CUDART_NAN_F : __uint_as_float(c & 0x80000000u ? c ^ 0x80000000u : ~c); }
+typedef unsigned long long code64;
+__device__ __forceinline__ code64 code_of(double f) {
+  const code64 u = static_cast<code64>(__double_as_longlong(f + 0.0));
+  return f != f ? NAN_CODE : u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+__device__ __forceinline__ double value_of(code64 c) {
+  return c <= NAN_CODE ? CUDART_NAN : __longlong_as_double(static_cast<long long>(c >> 63 ? c & 0x7FFFFFFFFFFFFFFFull : ~c));
+}
+__device__ __forceinline__ uint32_t largest(uint32_t c) { return __reduce_max_sync(0xffffffffu, c); }
+__device__ __forceinline__ code64 largest(code64 c) {
+  const uint32_t hi = static_cast<uint32_t>(c >> 32), top = largest(hi), low = largest(hi == top ? static_cast<uint32_t>(c) : 0u);
+  return static_cast<code64>(top) << 32 | low;
+}
 
 template <typename F> __device__ __forceinline__ F warp_sum(F x) {
 #pragma unroll
@@ -83,198 +81,463 @@ __device__ __forceinline__ float logit(const bf16* row, int e) { return __bfloat
 __device__ __forceinline__ float logit(const float* row, int e) { return row[e]; }
 
 // 1 / (1 + exp(-z)), without an exponential that overflows.
-template <typename F> __device__ __forceinline__ F sigmoid(F z) {
-  const F t = Code<F>::exponential(z < F(0) ? z : -z);
-  return (z < F(0) ? t : F(1)) / (F(1) + t);
+__device__ __forceinline__ float sigmoid(float z) {
+  const float t = expf(-fabsf(z));
+  return __fdividef(z < 0.f ? t : 1.f, 1.f + t);
+}
+__device__ __forceinline__ double sigmoid(double z) {
+  const double t = exp(-fabs(z));
+  return (z < 0.0 ? t : 1.0) / (1.0 + t);
+}
+// Scores in steps of 2^-30, and how far they can be off.  small: what the score, or one minus the score, has, to 4e-7 of itself (the exponential
+// an ulp, 1 + t half of one, its reciprocal one, the product half of one; a softmax has the error of its sum besides, 1.3e-6 common to all).
+constexpr float STEPS = 1073741824.f;
+__device__ __forceinline__ uint32_t steps_of(float small, bool lacks) {
+  const uint32_t n = __float2uint_rn(small * STEPS);
+  return lacks ? (1u << 30) - n : n;
+}
+__device__ __forceinline__ float sigmoid_small(float z) {      // min(sigmoid(z), sigmoid(-z))
+  float r;
+  const float t = expf(-fabsf(z));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + t));
+  return t * r;
 }
 
-// A token's choice: lane j < chosen has the j-th expert.  l: the logits of experts i * 32 + lane (-inf behind the last).
-// top, total: the largest logit and the sum of exp(l - top), where a softmax needs them.
-template <typename F> struct Choice { int id, chosen; float top; F total; bool unsure; };
+// Which of the groups stay: lane l has the score of group l >> shift; equal ones by rising index.
+template <typename C> __device__ __forceinline__ bool among_best(C mine, int shift, int top_groups, int lane) {
+  bool keep = false;
+  for (int j = 0; j < top_groups; ++j) {
+    const C left = keep ? 0 : mine, first = largest(left);
+    if (!first) break;
+    if ((__ffs(__ballot_sync(0xffffffffu, left == first)) - 1) >> shift == lane >> shift) keep = true;
+  }
+  return keep;
+}
 
-template <typename F, int NPL, typename T>
-__device__ __forceinline__ Choice<F> choose(const Route& p, const T* row, const float (&l)[NPL], int lane) {
-  typedef typename Code<F>::type code;
-  constexpr bool FLOAT = sizeof(F) == 4;
-  const bool scored = p.bias || (p.G > 1 && p.best == 2);      // whether the choice needs more than the order of the logits
-  Choice<F> c;
-  c.unsure = false;
-  c.top = -CUDART_INF_F;
-  c.total = F(1);
+// Scores in double, for what lies too near to each other for floats.  One exponential and one quotient for both kinds: this code is met
+// seldom and then cold.
+struct Exact { float top; double total; };
+template <typename T> __device__ __noinline__ double exact_score(const Exact x, bool by_sigmoid, float z) {
+  const double t = exp(by_sigmoid ? -fabs(static_cast<double>(z)) : static_cast<double>(z) - x.top);
+  return (by_sigmoid && z >= 0.f ? 1.0 : t) / (by_sigmoid ? 1.0 + t : x.total);
+}
+template <typename T> __device__ __noinline__ Exact exact_sum(const Route& p, const T* row, int lane) {
+  Exact x{-CUDART_INF_F, 1.0};
+  if (p.sigmoid) return x;
+  for (int e = lane; e < p.E; e += 32) x.top = fmaxf(x.top, logit(row, e));
+  x.top = warp_max(x.top);
+  double sum = 0.0;
+#pragma unroll 1
+  for (int e = lane; e < p.E; e += 32)
+    if (logit(row, e) != -CUDART_INF_F) sum += exact_score<T>(x, false, logit(row, e));
+  x.total = warp_sum(sum);
+  return x;
+}
+
+// The whole choice in double: lane j gets the j-th expert, or -1.
+template <typename T>
+__device__ __noinline__ int choose_exactly(const Route& p, const T* row, const float* bias, int lane) {
+  const bool by_two = p.G > 1 && p.best == 2, by_score = by_two && !p.bias;
+  const int per = (p.E + 31) / 32, first_e = lane * per;
+  code64 key[MAX_E / 32], count[MAX_E / 32];                   // what is chosen by, what a group counts: in local memory
+  const Exact x = p.bias || by_score ? exact_sum(p, row, lane) : Exact{};
+#pragma unroll 1
+  for (int i = 0; i < per; ++i) {
+    const int e = first_e + i;
+    key[i] = count[i] = 0;
+    if (e >= p.E) continue;
+    const float z = logit(row, e);
+    if (z == -CUDART_INF_F) continue;
+    const double s = p.bias || by_score ? exact_score<T>(x, p.sigmoid, z) : 0.0;
+    const double v = p.bias ? s + static_cast<double>(bias[e]) : z;
+    if (v == -CUDART_INF) continue;
+    key[i] = code_of(v);
+    count[i] = by_score ? code_of(s) : key[i];
+  }
+  if (p.G > 1) {
+    const int S = p.E / p.G;
+    code64 mine = 0;                                           // lane g: the score of group g
+#pragma unroll 1
+    for (int g = 0; g < p.G; ++g) {
+      code64 a = 0, b = 0;                                     // this lane's two best of the group
+      const int from = max(g * S - first_e, 0), to = min(g * S + S - first_e, per);
+#pragma unroll 1
+      for (int i = from; i < to; ++i) {
+        const code64 v = count[i];
+        if (v > a) { b = a; a = v; }
+        else if (v > b) b = v;
+      }
+      const code64 first = largest(a);
+      code64 of = first;
+      if (p.best == 2 && first) {
+        const unsigned owners = __ballot_sync(0xffffffffu, a == first);
+        const code64 second = largest(lane == __ffs(owners) - 1 ? b : a);
+        of = code_of(value_of(first) + (second ? value_of(second) : 0.0));
+      }
+      if (lane == g) mine = of;
+    }
+    const unsigned kept = __ballot_sync(0xffffffffu, among_best(mine, 0, p.top_groups, lane));
+#pragma unroll 1
+    for (int i = 0; i < per; ++i)
+      if (first_e + i < p.E && !(kept >> (first_e + i) / S & 1u)) key[i] = 0;
+  }
+  int id = -1;
+#pragma unroll 1
+  for (int j = 0; j < p.k; ++j) {
+    code64 best = 0;
+    int at = 0;
+#pragma unroll 1
+    for (int i = 0; i < per; ++i)
+      if (key[i] > best) { best = key[i]; at = i; }
+    const code64 first = largest(best);
+    if (!first) break;
+    const int src = __ffs(__ballot_sync(0xffffffffu, best == first)) - 1;
+    if (lane == src) key[at] = 0;
+    const int e = __shfl_sync(0xffffffffu, first_e + at, src);
+    if (lane == j) id = e;
+  }
+  return id;
+}
+
+// The order of n experts (lane j < n has one, `id`) whose keys lie near to each other, in double: lane j gets the j-th.
+template <typename T>
+__device__ __noinline__ int settle(const Route& p, const T* row, const float* bias, int id, int n, int lane) {
+  const float z = lane < n ? logit(row, id) : 0.f;
+  double v = z;
+  if (p.bias) v = exact_score<T>(exact_sum(p, row, lane), p.sigmoid, z) + (lane < n ? static_cast<double>(bias[id]) : 0.0);
+  const code64 mine = code_of(v);
+  int rank = 0;
+  for (int j = 0; j < n; ++j) {
+    const code64 other = __shfl_sync(0xffffffffu, mine, j);
+    const int e = __shfl_sync(0xffffffffu, id, j);
+    rank += other > mine || (other == mine && e < id);
+  }
+  int got = -1;
+  for (int j = 0; j < n; ++j) {
+    const int src = __ffs(__ballot_sync(0xffffffffu, lane < n && rank == j)) - 1;
+    const int e = __shfl_sync(0xffffffffu, id, src);
+    if (lane == j) got = e;
+  }
+  return got;
+}
+
+// NPL logits of lane `lane`, experts lane * NPL on; -inf behind the last.
+template <int NPL, typename T>
+__device__ __forceinline__ void logits_of(const T* row, int E, bool whole, int lane, float (&l)[NPL]) {
+  const int first = lane * NPL;
+  if (NPL * sizeof(T) >= 4 && whole) {                         // whole runs of NPL, aligned
+    if (first >= E) {
+#pragma unroll
+      for (int i = 0; i < NPL; ++i) l[i] = -CUDART_INF_F;
+      return;
+    }
+    constexpr int WORDS = NPL * static_cast<int>(sizeof(T)) / 4 > 0 ? NPL * static_cast<int>(sizeof(T)) / 4 : 1;
+    uint32_t w[WORDS];
+    const uint32_t* at = reinterpret_cast<const uint32_t*>(row + first);
+    if constexpr (WORDS >= 4) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(at + i);
+        w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+      }
+    } else if constexpr (WORDS == 2) {
+      const uint2 v = *reinterpret_cast<const uint2*>(at);
+      w[0] = v.x; w[1] = v.y;
+    } else {
+      w[0] = *at;
+    }
+#pragma unroll
+    for (int i = 0; i < NPL; ++i)
+      l[i] = __uint_as_float(sizeof(T) == 4 ? w[i] : i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) l[i] = first + i < E ? logit(row, first + i) : -CUDART_INF_F;
+  }
+}
+
+__device__ __forceinline__ void order(uint32_t& a, uint32_t& b) {
+  const uint32_t hi = max(a, b);
+  b = min(a, b);
+  a = hi;
+}
+// Falling order, by Batcher's odd-even merges.
+template <int N> __device__ __forceinline__ void sort_falling(uint32_t (&s)[N]) {
+#pragma unroll
+  for (int p = 1; p < N; p *= 2)
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = k % p; j + k < N; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) order(s[i + j], s[i + j + k]);
+}
+
+// A token's choice: lane j < chosen has the j-th expert.  top, total: the largest logit and the sum of exp(l - top), where a
+// softmax needs them.
+struct Choice { int id; float z, top, total; bool unsure; };          // z: the logit of expert id
+
+// Keys with a bias: fixed if all biases are within 0.99, (score + bias + 1) 2^30, the biases' share in shared memory; else the float sum's code.
+template <int NPL, typename T>
+__device__ __forceinline__ Choice choose(const Route& p, const T* row, const float (&l)[NPL], const float* bias, const uint32_t* bias_steps, bool fixed, int lane) {
+  constexpr uint32_t LOW = NPL - 1;
+  const bool by_two = p.G > 1 && p.best == 2, scored = p.bias || by_two;      // whether the choice needs more than the order of the logits
+  Choice c{-1, 0.f, -CUDART_INF_F, 1.f, false};
   if (!p.sigmoid && (scored || !p.renorm)) {
 #pragma unroll
     for (int i = 0; i < NPL; ++i) c.top = fmaxf(c.top, l[i]);
     c.top = warp_max(c.top);
-    F sum = F(0);
+    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NPL; ++i)
-      if (l[i] != -CUDART_INF_F) sum += Code<F>::exponential(F(l[i]) - F(c.top));
+      if (l[i] != -CUDART_INF_F) sum += expf(l[i] - c.top);
     c.total = warp_sum(sum);
   }
-  auto score = [&](float z) { return p.sigmoid ? sigmoid(F(z)) : Code<F>::exponential(F(z) - F(c.top)) / c.total; };
-  code key[NPL];
+  const float inv_total = p.sigmoid ? 1.f : __fdividef(1.f, c.total);
+  auto small = [&](float z) { return p.sigmoid ? sigmoid_small(z) : expf(z - c.top) * inv_total; };
+  auto steps = [&](float z) { return z != z || inv_total != inv_total ? NAN_CODE : (1u << 30) + steps_of(small(z), p.sigmoid && z >= 0.f); };
+  uint32_t key[NPL];
+  if (p.bias && fixed) {
 #pragma unroll
-  for (int i = 0; i < NPL; ++i) {
-    const int e = i * 32 + lane;
-    key[i] = 0;
-    if (l[i] != -CUDART_INF_F) {                               // (so e < E)
-      const F v = p.bias ? score(l[i]) + F(p.bias[e]) : F(l[i]);
-      if (v != F(-CUDART_INF)) key[i] = Code<F>::of(v);
+    for (int i = 0; i < NPL; ++i) {
+      key[i] = 0;
+      if (l[i] != -CUDART_INF_F) {                             // (so the expert exists)
+        const uint32_t s = steps(l[i]);
+        key[i] = ((s == NAN_CODE ? s : s + bias_steps[lane * NPL + i]) & ~LOW) | (LOW - i);
+      }
     }
+  } else if (p.bias) {
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) {
+      key[i] = 0;
+      if (l[i] != -CUDART_INF_F) {
+        const float s = small(l[i]), v = (p.sigmoid && l[i] >= 0.f ? 1.f - s : s) + bias[lane * NPL + i];
+        if (v != -CUDART_INF_F) key[i] = (code_of(v) & ~LOW) | (LOW - i);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) key[i] = l[i] != -CUDART_INF_F ? (code_of(l[i]) & ~LOW) | (LOW - i) : 0u;
   }
-  // how far float scores, and with them gaps between keys, can be off: the exponentials, the sum of up to 512 of them, the
-  // quotient (3e-6 of the largest p; 1e-6 for a sigmoid), and the sum with the bias
-  const float slack = p.sigmoid ? 1e-6f : 3e-6f / static_cast<float>(c.total);
+  sort_falling(key);
+  // How far the gap between two keys can be off, in steps or (keys that are sums of floats) by value.  Of a score: 4e-7 of the largest small
+  // part there is, a half or the largest p, whose sum's error counts with it; the steps' rounding and the bits given away.
+  const float part = p.sigmoid ? 0.5f : inv_total;
+  const float relative = p.sigmoid ? 4e-7f : 2e-6f, coarse = 2.f * relative * part;
   if (p.G > 1) {
-    const bool by_score = p.best == 2 && !p.bias;
-    code mine = 0;                                             // lane g: the score of group g
-    for (int g = 0; g < p.G; ++g) {
-      code a = 0, b = 0;                                       // this lane's two best of the group
+    const bool by_score = by_two && !p.bias, sums = by_two && (fixed || by_score);
+    // a lane's two best of a group, as the group counts them
+    auto counted = [&](uint32_t k) { return by_score && k ? steps(logit(row, lane * NPL + static_cast<int>(LOW - (k & LOW)))) : k & ~LOW; };
+    auto group_score = [&](uint32_t first, uint32_t second) {
+      if (p.best == 1 || !first) return first;
+      if (first <= 2 * NAN_CODE || (second && second <= 2 * NAN_CODE)) return NAN_CODE;
+      if (sums) return first / 2 + (second ? second / 2 : 1u << 29);             // (both have one in front)
+      return code_of(value_of(first) + (second ? value_of(second) : 0.f));
+    };
+    uint32_t mine;                                             // the score of this lane's group, or of group `lane`
+    bool keep;
+    if (p.group_lanes) {                                       // a lane has experts of one group, a group 1, 2, 4 .. lanes
+      uint32_t a = counted(key[0]), b = NPL > 1 ? counted(key[NPL > 1 ? 1 : 0]) : 0u;
+      for (int d = 1; d < 1 << (p.group_lanes - 1); d *= 2) {
+        const uint32_t a2 = __shfl_xor_sync(0xffffffffu, a, d), b2 = __shfl_xor_sync(0xffffffffu, b, d);
+        b = max(min(a, a2), max(b, b2));
+        a = max(a, a2);
+      }
+      mine = group_score(a, b);
+      keep = among_best(mine, p.group_lanes - 1, p.top_groups, lane);
+      if (!keep) {
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) key[i] = 0;
+      }
+    } else {
+      mine = 0;
+      for (int g = 0; g < p.G; ++g) {
+        uint32_t a = 0, b = 0;
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) {
+          const int e = lane * NPL + static_cast<int>(LOW - (key[i] & LOW));
+          if (key[i] == 0 || static_cast<int>(e * p.by_group >> 20) != g) continue;
+          const uint32_t v = counted(key[i]);
+          if (v > a) { b = a; a = v; }
+          else if (v > b) b = v;
+        }
+        const uint32_t first = largest(a), owners = __ballot_sync(0xffffffffu, a == first);
+        const uint32_t second = largest(lane == __ffs(owners) - 1 ? b : a);
+        if (lane == g) mine = group_score(first, second);
+      }
+      keep = among_best(mine, 0, p.top_groups, lane);          // (lanes behind the last group have 0)
+      const unsigned kept = __ballot_sync(0xffffffffu, keep);
 #pragma unroll
       for (int i = 0; i < NPL; ++i) {
-        const int e = i * 32 + lane;
-        if (key[i] == 0 || static_cast<int>(e * p.by_group >> 20) != g) continue;
-        const code v = by_score ? Code<F>::of(score(l[i])) : key[i];
-        if (v > a) { b = a; a = v; }
-        else if (v > b) b = v;
+        const int e = lane * NPL + static_cast<int>(LOW - (key[i] & LOW));
+        if (!(kept >> (e * p.by_group >> 20 & 31u) & 1u)) key[i] = 0;
       }
-      const code first = Code<F>::largest(a);
-      code of = first;
-      if (p.best == 2 && first) {
-        const unsigned owners = __ballot_sync(0xffffffffu, a == first);
-        const code second = Code<F>::largest(lane == __ffs(owners) - 1 ? b : a);
-        of = Code<F>::of(Code<F>::value(first) + (second ? Code<F>::value(second) : F(0)));
-      }
-      if (lane == g) mine = of;
+      sort_falling(key);
     }
-    int rank = 0;
-    for (int g = 0; g < p.G; ++g) {
-      const code other = __shfl_sync(0xffffffffu, mine, g);
-      rank += other > mine || (other == mine && g < lane);
-    }
-    const bool keep = lane < p.G && mine && rank < p.top_groups;
-    const unsigned kept = __ballot_sync(0xffffffffu, keep);
-    if (FLOAT && scored) {
-      const code out = Code<F>::largest(keep ? 0 : mine);      // (lanes behind the last group hold 0)
-      const code in = ~Code<F>::largest(keep ? ~mine : 0);
-      if (out && kept) {
-        const F a = Code<F>::value(in), b = Code<F>::value(out);
-        c.unsure = !(a - b > 2.f * slack + 6e-7f * fabsf(static_cast<float>(a)));
+    const uint32_t in = ~largest(keep ? ~mine : 0u), out = largest(keep ? 0u : mine);
+    if (out && in != ~0u) {
+      // (two groups of equal logits, by their best: the lower one, as it should be, if the bits given away are zeros anyway)
+      if (!scored) c.unsure = sizeof(T) == 4 && in == out;
+      else if (fixed || by_score)                              // (of two: twice as far off, in steps twice as long)
+        c.unsure = out <= 2 * NAN_CODE || in - out <= static_cast<uint32_t>(coarse * STEPS) + 2 * NPL + 4;
+      else {
+        const float a = value_of(in), b = value_of(out);
+        c.unsure = !(a - b > 2.f * coarse + 2.f * (NPL + 2) * 1.2e-7f * fabsf(a));
       }
     }
-#pragma unroll
-    for (int i = 0; i < NPL; ++i)
-      if (!(kept >> ((i * 32 + lane) * p.by_group >> 20 & 31u) & 1u)) key[i] = 0;       // (experts behind the last are not there anyway)
   }
-  c.id = -1;
-  c.chosen = 0;
-  code mine = 0;
+  uint32_t mine = 0;
+  int chosen = 0;
   for (int j = 0; j < p.k; ++j) {
-    code best = 0;
-#pragma unroll
-    for (int i = 0; i < NPL; ++i) best = key[i] > best ? key[i] : best;
-    const code top = Code<F>::largest(best);
-    if (!top) break;
-    int e = MAX_E;
-#pragma unroll
-    for (int i = NPL - 1; i >= 0; --i)
-      if (key[i] == top) e = i * 32 + lane;
-    e = __reduce_min_sync(0xffffffffu, e);
-#pragma unroll
-    for (int i = 0; i < NPL; ++i)
-      if (e == i * 32 + lane) key[i] = 0;
-    if (lane == j) { c.id = e; mine = top; }
-    c.chosen = j + 1;
-  }
-  if (FLOAT && p.bias && !c.unsure) {
-    // neighbours in the order, and the last one against all that are left; equal logits with equal biases are really equal
-    const float z = c.id >= 0 ? logit(row, c.id) : 0.f, b = c.id >= 0 ? p.bias[c.id] : 0.f, v = static_cast<float>(Code<F>::value(mine));
-    const float z2 = __shfl_down_sync(0xffffffffu, z, 1), b2 = __shfl_down_sync(0xffffffffu, b, 1), v2 = __shfl_down_sync(0xffffffffu, v, 1);
-    bool near = lane + 1 < c.chosen && !(v - v2 > slack + 3e-7f * fabsf(v)) && !(z == z2 && b == b2);
-    if (c.chosen == p.k) {
-      const float zk = __shfl_sync(0xffffffffu, z, p.k - 1), bk = __shfl_sync(0xffffffffu, b, p.k - 1), vk = __shfl_sync(0xffffffffu, v, p.k - 1);
-#pragma unroll
-      for (int i = 0; i < NPL; ++i)
-        if (key[i]) near |= !(vk - static_cast<float>(Code<F>::value(key[i])) > slack + 3e-7f * fabsf(vk)) && !(l[i] == zk && p.bias[i * 32 + lane] == bk);
+    const uint32_t own = key[0] & ~LOW, first = largest(own);
+    if (!first) break;
+    const int src = __ffs(__ballot_sync(0xffffffffu, own == first)) - 1;
+    const uint32_t got = __shfl_sync(0xffffffffu, key[0], src);
+    if (lane == j) {
+      mine = first;
+      c.id = src * NPL + static_cast<int>(LOW - (got & LOW));
     }
-    c.unsure = __any_sync(0xffffffffu, near);
+    if (lane == src) {
+#pragma unroll
+      for (int i = 0; i + 1 < NPL; ++i) key[i] = key[i + 1];
+      key[NPL - 1] = 0;
+    }
+    chosen = j + 1;
+  }
+  if (c.id >= 0) c.z = logit(row, c.id);
+  if (!p.bias && sizeof(T) == 2) return c;                     // (logits of bf16 end in zeros: nothing was given away)
+  if (c.unsure) return c;
+  // Neighbours in the order, and the last one against those that are left; equal logits with equal biases are really equal.  A first look by
+  // the largest error there can be, a second one by the two experts' own small parts.
+  const float value = p.bias && !fixed ? value_of(mine) : 0.f;
+  const uint32_t reach = p.bias && fixed ? static_cast<uint32_t>(coarse * STEPS) + NPL + 4 : 0u;
+  const float reach_value = coarse + (NPL + 2) * 1.2e-7f * fabsf(value);
+  auto close = [&](uint32_t hi, uint32_t lo, float value_hi, float within) {
+    if (hi <= 2 * NAN_CODE || lo <= 2 * NAN_CODE) return true;
+    return p.bias && !fixed ? !(value_hi - value_of(lo) > within) : hi - lo <= reach;
+  };
+  const uint32_t next = __shfl_down_sync(0xffffffffu, mine, 1);
+  const uint32_t last = __shfl_sync(0xffffffffu, mine, p.k - 1), left = key[0] & ~LOW;
+  const float value_last = __shfl_sync(0xffffffffu, value, p.k - 1), reach_last = __shfl_sync(0xffffffffu, reach_value, p.k - 1);
+  const bool near_next = lane + 1 < chosen && close(mine, next, value, reach_value);
+  const bool near_left = chosen == p.k && left && close(last, left, value_last, reach_last);
+  if (__any_sync(0xffffffffu, near_next || near_left)) {
+    const float z = c.z, b = c.id >= 0 && p.bias ? bias[c.id] : 0.f, s = p.bias && fixed && c.id >= 0 ? small(z) : 0.f;
+    auto differ = [&](uint32_t hi, uint32_t lo, float z1, float b1, float s1, float z2, float b2, float s2) {
+      if (z1 == z2 && b1 == b2) return false;
+      if (!(p.bias && fixed) || hi <= 2 * NAN_CODE || lo <= 2 * NAN_CODE) return true;
+      return hi - lo <= static_cast<uint32_t>(relative * (s1 + s2) * STEPS) + NPL + 4;
+    };
+    const float z2 = __shfl_down_sync(0xffffffffu, z, 1), b2 = __shfl_down_sync(0xffffffffu, b, 1), s2 = __shfl_down_sync(0xffffffffu, s, 1);
+    bool near = near_next && differ(mine, next, z, b, s, z2, b2, s2);
+    int n = chosen, id = c.id;                                 // with the keys that are left and near to the last one
+    if (__any_sync(0xffffffffu, near_left)) {
+      const float zk = __shfl_sync(0xffffffffu, z, p.k - 1), bk = __shfl_sync(0xffffffffu, b, p.k - 1), sk = __shfl_sync(0xffffffffu, s, p.k - 1);
+#pragma unroll
+      for (int i = 0; i < NPL; ++i) {
+        const int e = lane * NPL + static_cast<int>(LOW - (key[i] & LOW));
+        const bool may = key[i] && close(last, key[i] & ~LOW, value_last, reach_last);
+        if (may) {
+          const float ze = logit(row, e);
+          near |= differ(last, key[i] & ~LOW, zk, bk, sk, ze, p.bias ? bias[e] : 0.f, p.bias && fixed ? small(ze) : 0.f);
+        }
+        for (unsigned who = __ballot_sync(0xffffffffu, may); who; who &= who - 1) {
+          const int other = __shfl_sync(0xffffffffu, e, __ffs(who) - 1);
+          if (lane == n) id = other;
+          ++n;
+        }
+      }
+    }
+    if (__any_sync(0xffffffffu, near)) {
+      c.unsure = n > 32;
+      if (!c.unsure) {
+        id = settle(p, row, bias, id, n, lane);
+        c.id = lane < chosen ? id : -1;
+        c.z = c.id >= 0 ? logit(row, c.id) : 0.f;
+      }
+    }
   }
   return c;
-}
-
-template <int NPL, typename T>
-__device__ __forceinline__ void logits_of(const Route& p, const T* row, int lane, float (&l)[NPL]) {
-#pragma unroll
-  for (int i = 0; i < NPL; ++i) l[i] = i * 32 + lane < p.E ? logit(row, i * 32 + lane) : -CUDART_INF_F;
-}
-
-// The choice between values that lie too near to each other for floats.
-template <int NPL, typename T>
-__device__ __noinline__ int2 choose_in_double(const Route& p, const T* row, int lane) {
-  float l[NPL];
-  logits_of<NPL>(p, row, lane, l);
-  const Choice<double> c = choose<double, NPL>(p, row, l, lane);
-  return make_int2(c.id, c.chosen);
 }
 
 // The weight of lane j's expert, of logit z; total: over all experts.  Renormalised scores are taken relative to the largest
 // chosen one, so that scores below float's range keep their ratios: sigmoid(z) is exp(z) far below zero.
 __device__ __forceinline__ float share(float z, bool there, bool by_sigmoid, bool renorm, float top, float total) {
-  if (!renorm) return there ? (by_sigmoid ? sigmoid(z) : __fdiv_rn(expf(z - top), total)) : 0.f;
+  if (!renorm) return there ? (by_sigmoid ? sigmoid(z) : __fdividef(expf(z - top), total)) : 0.f;
   const float most = warp_max(there ? z : -CUDART_INF_F);
   const float r = !there || z == -CUDART_INF_F ? 0.f : by_sigmoid && !(most < -60.f) ? sigmoid(z) : expf(z - most);
   const float sum = warp_sum(r);
-  return there && sum != 0.f ? __fdiv_rn(r, sum) : 0.f;
+  return there && sum != 0.f ? __fdividef(r, sum) : 0.f;
 }
 
-// Exclusive sums of E numbers in shared memory, by one warp; all of them go behind the last.
-__device__ __forceinline__ void offsets_of(int* n, int E, int lane) {
-  const int per = (E + 31) / 32, first = lane * per;
-  int sum = 0;
-  for (int i = 0; i < per; ++i)
-    if (first + i < E) sum += n[first + i];
-  int before = sum;
+// Exclusive sums of E numbers in shared memory, by a block of at least as many threads; all of them go behind the last.
+__device__ __forceinline__ void offsets_of(int* n, int E) {
+  __shared__ int totals[32];
+  const int e = threadIdx.x, lane = e & 31, warp = e >> 5, own = e < E ? n[e] : 0;
+  int sum = own;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, before, d);
-    if (lane >= d) before += v;
+    const int v = __shfl_up_sync(0xffffffffu, sum, d);
+    if (lane >= d) sum += v;
   }
-  if (lane == 31) n[E] = before;
-  before -= sum;
-  for (int i = 0; i < per; ++i)
-    if (first + i < E) {
-      const int v = n[first + i];
-      n[first + i] = before;
-      before += v;
-    }
+  if (lane == 31) totals[warp] = sum;
+  __syncthreads();
+  if (e < E) {
+#pragma unroll
+    for (int w = 0; w < MAX_E / 32 - 1; ++w)
+      if (w < warp) sum += totals[w];
+    n[e] = sum - own;
+    if (e == E - 1) n[E] = sum;
+  }
+  __syncthreads();
 }
 
-template <typename T, int NPL>
-__global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Route p) {
+template <typename T, int NPL, int MAXT>
+__global__ void __launch_bounds__(MAXT) route_kernel(const __grid_constant__ Route p) {
   __shared__ uint32_t chose[MAX_E][SUB / 32];
   __shared__ int running[MAX_E + 1];
   __shared__ int16_t ids[SUB * MAX_K];
+  __shared__ __align__(16) float bias[MAX_E];
+  __shared__ __align__(16) uint32_t bias_steps[MAX_E];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   pdl_trigger();
   pdl_wait();
   const int live = p.count ? min(max(*p.count, 0), p.T) : p.T;
-  for (int e = threadIdx.x; e <= p.E; e += blockDim.x) running[e] = 0;
+  int fits = 1;
+  for (int e = threadIdx.x; e <= p.E; e += blockDim.x) {
+    running[e] = 0;
+    if (p.bias && e < p.E) {
+      const float b = p.bias[e];
+      bias[e] = b;
+      fits &= fabsf(b) <= 0.99f;
+      bias_steps[e] = static_cast<uint32_t>(__float2int_rn(b * STEPS));        // (exact but for the rounding to a step; negative ones wrap around)
+    }
+  }
+  const bool fixed = __syncthreads_and(fits);
   const int64_t begin = blockIdx.x * static_cast<int64_t>(p.chunk), end = min(begin + p.chunk, static_cast<int64_t>(p.T));
   for (int64_t sub = begin; sub < end; sub += SUB) {
     for (int e = threadIdx.x; e < p.E * (SUB / 32); e += blockDim.x) chose[0][e] = 0u;
     __syncthreads();
     const int tokens = static_cast<int>(min(end - sub, static_cast<int64_t>(SUB)));
+    float next[NPL];                                           // the warp's next token is on its way
+    if (warp < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (sub + warp) * p.ld, p.E, p.whole, lane, next);
     for (int i = warp; i < tokens; i += warps) {
       const int64_t t = sub + i;
       int id = -1;
-      float w = 0.f;
+      float w = 0.f, l[NPL];
+#pragma unroll
+      for (int m = 0; m < NPL; ++m) l[m] = next[m];
+      if (i + warps < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (t + warps) * p.ld, p.E, p.whole, lane, next);
       if (t < live) {
         const T* row = static_cast<const T*>(p.logits) + t * p.ld;
-        float l[NPL];
-        logits_of<NPL>(p, row, lane, l);
-        const Choice<float> c = choose<float, NPL>(p, row, l, lane);
-        id = c.unsure ? choose_in_double<NPL>(p, row, lane).x : c.id;
-        w = share(id >= 0 ? logit(row, id) : 0.f, id >= 0, p.sigmoid, p.renorm, c.top, c.total) * p.scale;
+        const Choice c = choose<NPL>(p, row, l, bias, bias_steps, fixed, lane);
+        float z = c.z;
+        id = c.id;
+        if (c.unsure) {
+          id = choose_exactly(p, row, bias, lane);
+          z = id >= 0 ? logit(row, id) : 0.f;
+        }
+        w = share(z, id >= 0, p.sigmoid, p.renorm, c.top, c.total) * p.scale;
       }
       if (lane < p.k) {
         p.ids[t * p.k + lane] = id;
@@ -287,8 +550,7 @@ __global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Rou
     if (!p.counts) {                                           // the only block: the experts' first rows are known here
       for (int e = threadIdx.x; e < p.E; e += blockDim.x) running[e] = __popc(chose[e][0]) + __popc(chose[e][1]);
       __syncthreads();
-      if (warp == 0) offsets_of(running, p.E, lane);
-      __syncthreads();
+      offsets_of(running, p.E);
       for (int e = threadIdx.x; e <= p.E; e += blockDim.x) p.offsets[e] = running[e];
     }
     for (int s = threadIdx.x; s < tokens * p.k; s += blockDim.x) {
@@ -305,45 +567,60 @@ __global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Rou
     for (int e = threadIdx.x; e < p.E; e += blockDim.x) running[e] += __popc(chose[e][0]) + __popc(chose[e][1]);
     __syncthreads();
   }
-  for (int e = threadIdx.x; e < p.E2; e += blockDim.x) p.counts[blockIdx.x * static_cast<int64_t>(p.E2) + e] = e < p.E ? static_cast<uint16_t>(running[e]) : 0;
+  for (int e = threadIdx.x; e < p.E8; e += blockDim.x) p.counts[blockIdx.x * static_cast<int64_t>(p.E8) + e] = e < p.E ? static_cast<uint16_t>(running[e]) : 0;
 }
 
-// Each block adds up the blocks' counts: its experts' first rows, and what the blocks before it have.
+// Each block takes the slots of one block of the kernel above: it adds up all blocks' counts, which gives the experts' first rows, and those
+// of the blocks before its own; eight experts a thread, the blocks dealt out to STRANDS threads, all of whose loads are under way at once.
+constexpr int STRANDS = 8;
 __global__ void __launch_bounds__(512) places_kernel(const __grid_constant__ Route p) {
   __shared__ int total[MAX_E + 1], before[MAX_E];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ __align__(16) int all[STRANDS][MAX_E], earlier[STRANDS][MAX_E];
+  const int blocks = gridDim.x, own = blockIdx.x;
+  const int64_t begin = own * static_cast<int64_t>(p.chunk) * p.k, end = min((own + 1) * static_cast<int64_t>(p.chunk), static_cast<int64_t>(p.T)) * p.k;
   pdl_trigger();
   pdl_wait();
-  for (int e = threadIdx.x; e <= p.E; e += blockDim.x) {
-    total[e] = 0;
-    if (e < p.E) before[e] = 0;
+  const int64_t slot = begin + threadIdx.x;                    // the first of this thread's slots is on its way meanwhile
+  const int first_id = slot < end ? p.ids[slot] : -1, first_place = slot < end ? p.places[slot] : -1;
+  const int eights = p.E8 / 8, strand = threadIdx.x / eights, at = threadIdx.x - strand * eights;
+  if (strand < STRANDS) {
+    const uint4* counts = reinterpret_cast<const uint4*>(p.counts) + at;
+    int n[8] = {}, m[8] = {};
+#pragma unroll 10
+    for (int b = strand; b < blocks; b += STRANDS) {
+      const uint4 v = counts[b * static_cast<int64_t>(eights)];
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      const int before_own = b < own ? -1 : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = static_cast<int>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu);
+        n[i] += c;
+        m[i] += c & before_own;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      *reinterpret_cast<int4*>(&all[strand][8 * at + i]) = make_int4(n[i], n[i + 1], n[i + 2], n[i + 3]);
+      *reinterpret_cast<int4*>(&earlier[strand][8 * at + i]) = make_int4(m[i], m[i + 1], m[i + 2], m[i + 3]);
+    }
   }
   __syncthreads();
-  const int pairs = p.E2 / 2, strands = blockDim.x / pairs, strand = threadIdx.x / pairs, at = threadIdx.x - strand * pairs;
-  if (strand < strands) {
-    const uint32_t* counts = reinterpret_cast<const uint32_t*>(p.counts) + at;
-    int all0 = 0, all1 = 0, own0 = 0, own1 = 0;
-#pragma unroll 8
-    for (int b = strand; b < static_cast<int>(gridDim.x); b += strands) {
-      const uint32_t v = counts[b * static_cast<int64_t>(pairs)];
-      const int lo = static_cast<int>(v & 0xFFFFu), hi = static_cast<int>(v >> 16);
-      all0 += lo; all1 += hi;
-      if (b < static_cast<int>(blockIdx.x)) { own0 += lo; own1 += hi; }
+  for (int e = threadIdx.x; e < p.E; e += blockDim.x) {
+    int n = 0, m = 0;
+#pragma unroll
+    for (int s = 0; s < STRANDS; ++s) {
+      n += all[s][e];
+      m += earlier[s][e];
     }
-    atomicAdd(&total[2 * at], all0);
-    atomicAdd(&before[2 * at], own0);
-    if (2 * at + 1 < p.E) {
-      atomicAdd(&total[2 * at + 1], all1);
-      atomicAdd(&before[2 * at + 1], own1);
-    }
+    total[e] = n;
+    before[e] = m;
   }
   __syncthreads();
-  if (warp == 0) offsets_of(total, p.E, lane);
-  __syncthreads();
-  if (blockIdx.x == 0)
+  offsets_of(total, p.E);
+  if (own == 0)
     for (int e = threadIdx.x; e <= p.E; e += blockDim.x) p.offsets[e] = total[e];
-  const int64_t begin = blockIdx.x * static_cast<int64_t>(p.chunk), end = min(begin + p.chunk, static_cast<int64_t>(p.T));
-  for (int64_t s = begin * p.k + threadIdx.x; s < end * p.k; s += blockDim.x) {
+  if (first_id >= 0) p.places[slot] = first_place + total[first_id] + before[first_id];
+  for (int64_t s = slot + blockDim.x; s < end; s += blockDim.x) {
     const int e = p.ids[s];
     if (e >= 0) p.places[s] += total[e] + before[e];
   }
@@ -414,18 +691,30 @@ __global__ void __launch_bounds__(256) route_backward_kernel(const __grid_consta
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
+// Tokens of a block: 16 or more, but at most MOST_BLOCKS blocks, one per SM.
 int chunk_of(int64_t T) {
-  int64_t chunk = ((T + MOST_BLOCKS - 1) / MOST_BLOCKS + SUB - 1) / SUB * SUB;
+  int64_t chunk = ((T + MOST_BLOCKS - 1) / MOST_BLOCKS + 7) / 8 * 8;
+  if (chunk < 16) chunk = 16;
   return static_cast<int>(chunk < MOST_TOKENS ? chunk : MOST_TOKENS);
 }
 int64_t blocks_of(int64_t T) { return T <= SUB ? 1 : (T + chunk_of(T) - 1) / chunk_of(T); }
 
+template <typename T, int NPL> cudaError_t launch_npl(Route p, dim3 grid, dim3 block, cudaStream_t stream) {
+  constexpr uint64_t BYTES = NPL * sizeof(T) < 16 ? NPL * sizeof(T) : 16;
+  constexpr int MOST = NPL < 16 ? 1024 : 512;
+  p.whole = p.E % NPL == 0 && reinterpret_cast<uintptr_t>(p.logits) % BYTES == 0 && (p.T <= 1 || static_cast<uint64_t>(p.ld) * sizeof(T) % BYTES == 0);
+  const int S = p.E / p.G, lanes = S / NPL;
+  if (p.G > 1 && S % NPL == 0 && (lanes & (lanes - 1)) == 0)
+    for (p.group_lanes = 1; 1 << (p.group_lanes - 1) < lanes; ++p.group_lanes) {}
+  if (block.x > MOST) block.x = MOST;
+  return launch_pdl(route_kernel<T, NPL, MOST>, grid, block, 0, stream, 1, p);
+}
 template <typename T> cudaError_t launch(const Route& p, dim3 grid, dim3 block, cudaStream_t stream) {
-  if (p.E <= 32) return launch_pdl(route_kernel<T, 1>, grid, block, 0, stream, 1, p);
-  if (p.E <= 64) return launch_pdl(route_kernel<T, 2>, grid, block, 0, stream, 1, p);
-  if (p.E <= 128) return launch_pdl(route_kernel<T, 4>, grid, block, 0, stream, 1, p);
-  if (p.E <= 256) return launch_pdl(route_kernel<T, 8>, grid, block, 0, stream, 1, p);
-  return launch_pdl(route_kernel<T, 16>, grid, block, 0, stream, 1, p);
+  if (p.E <= 32) return launch_npl<T, 1>(p, grid, block, stream);
+  if (p.E <= 64) return launch_npl<T, 2>(p, grid, block, stream);
+  if (p.E <= 128) return launch_npl<T, 4>(p, grid, block, stream);
+  if (p.E <= 256) return launch_npl<T, 8>(p, grid, block, stream);
+  return launch_npl<T, 16>(p, grid, block, stream);
 }
 
 mbd_status done(cudaError_t e) {
@@ -449,7 +738,7 @@ using namespace mbd;
 
 extern "C" int64_t mbd_expert_route_scratch(int64_t T, int E) {
   if (T <= SUB || E < 1) return 0;
-  return blocks_of(T) * ((E + 1) / 2);
+  return blocks_of(T) * ((E + 7) / 8 * 4);
 }
 
 extern "C" mbd_status mbd_expert_route(const mbd_router* router, int64_t T, const void* logits_dev, int logits_bf16, int64_t ld, const float* bias_dev,
@@ -461,6 +750,7 @@ extern "C" mbd_status mbd_expert_route(const mbd_router* router, int64_t T, cons
   const int64_t words = mbd_expert_route_scratch(T, E);
   if (!offsets_dev || (T > 0 && (!logits_dev || !ids_dev || !weights_dev || !places_dev)) || (words && !scratch_dev)) return MBD_E_INVALID;
   if (T > 1 && ld < E) return MBD_E_INVALID;
+  if (words && reinterpret_cast<uintptr_t>(scratch_dev) % 16) return MBD_E_UNSUPPORTED;
   const Rows logits{T > 0 ? logits_dev : nullptr, T, E, ld, logits_bf16 ? 2 : 4}, bias{bias_dev, 1, E, E, 4}, count{count_dev, 1, 1, 1, 4};
   const Rows ids{T > 0 ? ids_dev : nullptr, 1, T * k, T * k, 4}, weights{T > 0 ? weights_dev : nullptr, 1, T * k, T * k, 4},
       places{T > 0 ? places_dev : nullptr, 1, T * k, T * k, 4}, offsets{offsets_dev, 1, E + 1, E + 1, 4}, scratch{words ? scratch_dev : nullptr, 1, words, words, 4};
@@ -480,10 +770,10 @@ extern "C" mbd_status mbd_expert_route(const mbd_router* router, int64_t T, cons
   const uint32_t S = static_cast<uint32_t>(E / router->groups);
   const bool one = T <= SUB;
   const Route p{logits_dev, bias_dev, count_dev, ids_dev, places_dev, offsets_dev, weights_dev, one ? nullptr : reinterpret_cast<uint16_t*>(scratch_dev), ld,
-                static_cast<int>(T), E, (E + 1) / 2 * 2, k, one ? SUB : chunk_of(T), router->score == MBD_ROUTE_SIGMOID, router->renormalise != 0,
-                router->groups, router->top_groups, router->group_best, ((1u << 20) + S - 1) / S, router->scale};
-  int warps = one ? 1 : 16;
-  while (one && warps < T && warps < 32) warps *= 2;
+                static_cast<int>(T), E, (E + 7) / 8 * 8, k, one ? SUB : chunk_of(T), 0, router->score == MBD_ROUTE_SIGMOID, router->renormalise != 0,
+                router->groups, router->top_groups, router->group_best, ((1u << 20) + S - 1) / S, 0, router->scale};
+  int warps = (E + 31) / 32;                                  // (a thread per expert at least)
+  while (warps < (one ? T : chunk_of(T)) && warps < 32) ++warps;
   const dim3 grid(static_cast<unsigned>(blocks_of(T))), block(32 * warps);
   const cudaError_t e = logits_bf16 ? launch<bf16>(p, grid, block, stream) : launch<float>(p, grid, block, stream);
   if (e != cudaSuccess || one) return done(e);
