@@ -85,10 +85,6 @@ __device__ __forceinline__ float sigmoid(float z) {
   const float t = expf(-fabsf(z));
   return __fdividef(z < 0.f ? t : 1.f, 1.f + t);
 }
-__device__ __forceinline__ double sigmoid(double z) {
-  const double t = exp(-fabs(z));
-  return (z < 0.0 ? t : 1.0) / (1.0 + t);
-}
 // Scores in steps of 2^-30, and how far they can be off.  small: what the score, or one minus the score, has, to 4e-7 of itself (the exponential
 // an ulp, 1 + t half of one, its reciprocal one, the product half of one; a softmax has the error of its sum besides, 1.3e-6 common to all).
 constexpr float STEPS = 1073741824.f;
@@ -492,8 +488,8 @@ __device__ __forceinline__ void offsets_of(int* n, int E) {
   __syncthreads();
 }
 
-template <typename T, int NPL, int MAXT>
-__global__ void __launch_bounds__(MAXT) route_kernel(const __grid_constant__ Route p) {
+template <typename T, int NPL>
+__global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Route p) {
   __shared__ uint32_t chose[MAX_E][SUB / 32];
   __shared__ int running[MAX_E + 1];
   __shared__ int16_t ids[SUB * MAX_K];
@@ -519,15 +515,17 @@ __global__ void __launch_bounds__(MAXT) route_kernel(const __grid_constant__ Rou
     for (int e = threadIdx.x; e < p.E * (SUB / 32); e += blockDim.x) chose[0][e] = 0u;
     __syncthreads();
     const int tokens = static_cast<int>(min(end - sub, static_cast<int64_t>(SUB)));
+    constexpr bool AHEAD = NPL < 16;                           // (with 16 more registers a thread 512 threads fit, not 1024: 16384 tokens of 512 experts 107 instead of 99 us)
     float next[NPL];                                           // the warp's next token is on its way
-    if (warp < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (sub + warp) * p.ld, p.E, p.whole, lane, next);
+    if (AHEAD && warp < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (sub + warp) * p.ld, p.E, p.whole, lane, next);
     for (int i = warp; i < tokens; i += warps) {
       const int64_t t = sub + i;
       int id = -1;
       float w = 0.f, l[NPL];
 #pragma unroll
-      for (int m = 0; m < NPL; ++m) l[m] = next[m];
-      if (i + warps < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (t + warps) * p.ld, p.E, p.whole, lane, next);
+      for (int m = 0; m < NPL; ++m) l[m] = AHEAD ? next[m] : 0.f;
+      if (!AHEAD) logits_of<NPL>(static_cast<const T*>(p.logits) + t * p.ld, p.E, p.whole, lane, l);
+      else if (i + warps < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (t + warps) * p.ld, p.E, p.whole, lane, next);
       if (t < live) {
         const T* row = static_cast<const T*>(p.logits) + t * p.ld;
         const Choice c = choose<NPL>(p, row, l, bias, bias_steps, fixed, lane);
@@ -633,14 +631,19 @@ struct RouteGrad {
   const float* d_weights;
   void* d_logits;
   int64_t ld, ldd;
-  int T, E, k, sigmoid, renorm, out_bf16;
+  int T, E, k, sigmoid, renorm, out_bf16, pairs;      // pairs: two elements of the result at a time
   float scale;
 };
 
+// One warp per token; its row of the result is put together in shared memory, the slots' shares one after the other (the same expert
+// named twice gets both).
+constexpr int GRAD_WARPS = 8;
 template <typename T>
-__global__ void __launch_bounds__(256) route_backward_kernel(const __grid_constant__ RouteGrad p) {
+__global__ void __launch_bounds__(32 * GRAD_WARPS) route_backward_kernel(const __grid_constant__ RouteGrad p) {
+  __shared__ __align__(16) float rows[GRAD_WARPS][MAX_E];
   const int lane = threadIdx.x & 31;
-  const int64_t t = blockIdx.x * static_cast<int64_t>(blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int64_t t = blockIdx.x * static_cast<int64_t>(GRAD_WARPS) + (threadIdx.x >> 5);
+  float* out = rows[threadIdx.x >> 5];
   pdl_trigger();
   pdl_wait();
   if (t >= p.T) return;
@@ -649,44 +652,54 @@ __global__ void __launch_bounds__(256) route_backward_kernel(const __grid_consta
   if (id >= p.E) id = -1;
   const bool there = id >= 0;
   const float z = there ? logit(row, id) : 0.f, dw = there ? p.d_weights[t * p.k + lane] * p.scale : 0.f;
-  float top = -CUDART_INF_F, total = 1.f, common = 0.f, own = 0.f;       // dl_e = -p_e common (softmax over all) + own of the slots with e
-  const bool all = !p.sigmoid && !p.renorm;
+  float top = -CUDART_INF_F, total = 1.f, own;
+  const bool all = !p.sigmoid && !p.renorm;              // every logit has a part: dl_e = own of the slots with e - p_e * (sum of own)
   if (all) {
-    for (int e = lane; e < p.E; e += 32) top = fmaxf(top, logit(row, e));
+    for (int e = lane; e < p.E; e += 32) {
+      const float l = logit(row, e);
+      out[e] = l;
+      top = fmaxf(top, l);
+    }
     top = warp_max(top);
     float sum = 0.f;
     for (int e = lane; e < p.E; e += 32) {
-      const float v = logit(row, e);
-      if (v != -CUDART_INF_F) sum += expf(v - top);
+      const float l = out[e], v = l == -CUDART_INF_F ? 0.f : expf(l - top);
+      out[e] = v;
+      sum += v;
     }
     total = warp_sum(sum);
   }
   const float s = share(z, there, p.sigmoid, p.renorm, top, total);
   if (all) {
-    const bool chosen = there && z != -CUDART_INF_F;
-    own = chosen ? s * dw : 0.f;
-    common = warp_sum(own);
+    own = there && z != -CUDART_INF_F ? s * dw : 0.f;
+    const float common = -__fdividef(warp_sum(own), total);
+    for (int e = lane; e < p.E; e += 32) out[e] = out[e] == 0.f ? 0.f : common * out[e];      // (a masked expert has none, whatever the total)
   } else {
     const float mean = p.renorm ? warp_sum(there ? s * dw : 0.f) : 0.f;
-    const float slope = p.sigmoid ? sigmoid(-z) : 1.f;  // (sigmoid(-z) = 1 - sigmoid(z))
+    const float slope = p.sigmoid ? sigmoid(-z) : 1.f;   // (sigmoid(-z) = 1 - sigmoid(z))
     own = there ? s * slope * (dw - mean) : 0.f;
+    for (int e = lane; e < p.E; e += 32) out[e] = 0.f;
   }
-  for (int first = 0; first < p.E; first += 32) {
-    const int e = first + lane;
-    float v = 0.f;
-    if (all && e < p.E) {
-      const float ze = logit(row, e);
-      v = ze == -CUDART_INF_F ? 0.f : -common * __fdiv_rn(expf(ze - top), total);
-    }
-    for (int j = 0; j < p.k; ++j) {                            // (the same expert named twice gets both)
-      const int ej = __shfl_sync(0xffffffffu, id, j);
-      const float x = __shfl_sync(0xffffffffu, own, j);
-      if (ej == e) v += x;
-    }
-    if (e < p.E) {
-      if (p.out_bf16) static_cast<bf16*>(p.d_logits)[t * p.ldd + e] = __float2bfloat16_rn(v);
-      else static_cast<float*>(p.d_logits)[t * p.ldd + e] = v;
-    }
+  __syncwarp();
+  for (int j = 0; j < p.k; ++j) {
+    if (lane == j && there) out[id] += own;
+    __syncwarp();
+  }
+  if (p.out_bf16) {
+    bf16* to = static_cast<bf16*>(p.d_logits) + t * p.ldd;
+    if (p.pairs)
+      for (int e = lane; e < p.E / 2; e += 32) {
+        const float2 v = *reinterpret_cast<const float2*>(out + 2 * e);
+        *reinterpret_cast<uint32_t*>(to + 2 * e) = pack_bf16x2(v.x, v.y);
+      }
+    else
+      for (int e = lane; e < p.E; e += 32) to[e] = __float2bfloat16_rn(out[e]);
+  } else {
+    float* to = static_cast<float*>(p.d_logits) + t * p.ldd;
+    if (p.pairs)
+      for (int e = lane; e < p.E / 2; e += 32) *reinterpret_cast<float2*>(to + 2 * e) = *reinterpret_cast<const float2*>(out + 2 * e);
+    else
+      for (int e = lane; e < p.E; e += 32) to[e] = out[e];
   }
 }
 
@@ -701,13 +714,11 @@ int64_t blocks_of(int64_t T) { return T <= SUB ? 1 : (T + chunk_of(T) - 1) / chu
 
 template <typename T, int NPL> cudaError_t launch_npl(Route p, dim3 grid, dim3 block, cudaStream_t stream) {
   constexpr uint64_t BYTES = NPL * sizeof(T) < 16 ? NPL * sizeof(T) : 16;
-  constexpr int MOST = NPL < 16 ? 1024 : 512;
   p.whole = p.E % NPL == 0 && reinterpret_cast<uintptr_t>(p.logits) % BYTES == 0 && (p.T <= 1 || static_cast<uint64_t>(p.ld) * sizeof(T) % BYTES == 0);
   const int S = p.E / p.G, lanes = S / NPL;
   if (p.G > 1 && S % NPL == 0 && (lanes & (lanes - 1)) == 0)
     for (p.group_lanes = 1; 1 << (p.group_lanes - 1) < lanes; ++p.group_lanes) {}
-  if (block.x > MOST) block.x = MOST;
-  return launch_pdl(route_kernel<T, NPL, MOST>, grid, block, 0, stream, 1, p);
+  return launch_pdl(route_kernel<T, NPL>, grid, block, 0, stream, 1, p);
 }
 template <typename T> cudaError_t launch(const Route& p, dim3 grid, dim3 block, cudaStream_t stream) {
   if (p.E <= 32) return launch_npl<T, 1>(p, grid, block, stream);
@@ -794,8 +805,9 @@ extern "C" mbd_status mbd_expert_route_backward(const mbd_router* router, int64_
     if (t->misplaced()) return MBD_E_UNSUPPORTED;
   if (!apart(out, logits) || !apart(out, ids) || !apart(out, dw)) return MBD_E_INVALID;
   const RouteGrad p{logits_dev, ids_dev, d_weights_dev, d_logits_dev, ld, ldd, static_cast<int>(T), E, k, router->score == MBD_ROUTE_SIGMOID,
-                    router->renormalise != 0, d_logits_bf16 != 0, router->scale};
-  const dim3 grid(static_cast<unsigned>((T + 7) / 8)), block(256);
+                    router->renormalise != 0, d_logits_bf16 != 0,
+                    E % 2 == 0 && (T == 1 || ldd % 2 == 0) && reinterpret_cast<uintptr_t>(d_logits_dev) % (2 * out.size) == 0, router->scale};
+  const dim3 grid(static_cast<unsigned>((T + GRAD_WARPS - 1) / GRAD_WARPS)), block(32 * GRAD_WARPS);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   return done(logits_bf16 ? launch_pdl(route_backward_kernel<bf16>, grid, block, 0, stream, 1, p)
                           : launch_pdl(route_backward_kernel<float>, grid, block, 0, stream, 1, p));
