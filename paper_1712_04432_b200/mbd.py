@@ -726,28 +726,24 @@ def expert_gemm_i8(A, a_scale, B, b_scale, offsets, out, relu: bool = False, bia
     return out
 
 
-def _float(dtype) -> bool:
-    """Whether a tensor of bf16 or float holds bf16."""
-    assert dtype == _t.bf16 or dtype == _t.f32
-    return dtype == _t.bf16
-
-
 def _rows_at(t, shape, dev: int):
-    """(address, is bf16, row stride) of a bf16 or float tensor of `shape` [rows, K]; (None, 0, 0) for None."""
+    """(address, is bf16, row stride) of a bf16 or float tensor of `shape` [rows, K] on the current device; (None, 0, 0) for None."""
     if t is None:
         return None, 0, 0
-    assert t.shape == shape
+    dtype = t.dtype
+    bf16 = dtype is _t.bf16
+    assert (bf16 or dtype is _t.f32) and t.shape == shape and t.get_device() == dev
     ld, one = t.stride()
     assert one == 1 or shape[1] == 1
-    return _at(t, dev), _float(t.dtype), (ld if shape[0] > 1 else shape[1])
+    return t.data_ptr(), bf16, ld if shape[0] > 1 else shape[1]
 
 
 def _dense(t, dtype, shape, dev: int):
-    """Address of a contiguous tensor, or None."""
+    """Address of a contiguous tensor on the current device, or None."""
     if t is None:
         return None
-    assert t.dtype == dtype and t.shape == shape and t.is_contiguous()
-    return _at(t, dev)
+    assert t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev
+    return t.data_ptr()
 
 
 def rms_norm(x, gain=None, residual=None, h=None, y=None, q=None, scale=None, eps: float = 1e-6):

@@ -28,7 +28,7 @@ BWD = dict(T=100, logits=1 * MB, bf16=0, ld=16, ids=2 * MB, dw=3 * MB, out=4 * M
     ({}, dict(T=-1), mbd.E_INVALID), ({}, dict(logits=None), mbd.E_INVALID), ({}, dict(ids=None), mbd.E_INVALID), ({}, dict(weights=None), mbd.E_INVALID),
     ({}, dict(places=None), mbd.E_INVALID), ({}, dict(offsets=None), mbd.E_INVALID), ({}, dict(scratch=None), mbd.E_INVALID), ({}, dict(ld=15), mbd.E_INVALID),
     ({}, dict(logits=1 * MB + 2), mbd.E_UNSUPPORTED), ({}, dict(logits=1 * MB + 1, bf16=1), mbd.E_UNSUPPORTED), ({}, dict(ids=4 * MB + 2), mbd.E_UNSUPPORTED),
-    ({}, dict(count=3 * MB + 2), mbd.E_UNSUPPORTED), ({}, dict(T=2 ** 27), mbd.E_UNSUPPORTED),
+    ({}, dict(count=3 * MB + 2), mbd.E_UNSUPPORTED), ({}, dict(scratch=8 * MB + 8), mbd.E_UNSUPPORTED), ({}, dict(T=2 ** 27), mbd.E_UNSUPPORTED),
     ({}, dict(places=4 * MB), mbd.E_INVALID), ({}, dict(weights=1 * MB + 64), mbd.E_INVALID), ({}, dict(offsets=6 * MB), mbd.E_INVALID),
     ({}, dict(ids=2 * MB), mbd.E_INVALID), ({}, dict(scratch=5 * MB + 16), mbd.E_INVALID), ({}, dict(offsets=3 * MB - 8), mbd.E_INVALID),
 ])
@@ -217,6 +217,37 @@ def test_keys_that_floats_cannot_tell_apart(score):
         rows = np.repeat(l[None], 40, 0)
         assert len(np.unique((p.astype(np.float32) + bias).astype(np.float32))) < E / 2
         _compare(mbd.Router(E, k, score, True, G, top, best), torch.from_numpy(rows).cuda(), torch.from_numpy(bias).cuda())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("level", [0.0, 0.6, 6.0])
+def test_pairs_of_keys_that_floats_cannot_tell_apart(score, level):
+    """Experts in pairs whose keys are a few 2^-26 apart, the pairs far from each other: at small biases, and at ones beyond one."""
+    import torch
+    rng = np.random.default_rng(int(level * 10) + score)
+    for E, k, G, top, best in ((64, 5, 1, 1, 1), (256, 8, 8, 4, 2), (100, 12, 4, 2, 1), (512, 32, 1, 1, 1)):
+        l = rng.normal(size=E).astype(np.float32)
+        p = _scores(l[None], score)[0]
+        bias = (level + 0.3 * rng.random(E)).astype(np.float32)
+        other = rng.permutation(E)
+        for a, b in zip(other[::2], other[1::2]):                    # b's key becomes a's, as near as a float bias goes
+            bias[b] = np.float32(p[a] + np.float64(bias[a]) - p[b])
+        rows = np.repeat(l[None], 30, 0)
+        _compare(mbd.Router(E, k, score, True, G, top, best), torch.from_numpy(rows).cuda(), torch.from_numpy(bias).cuda())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G,top,best", [(1, 1, 1), (8, 3, 1), (8, 3, 2), (5, 2, 1)])
+def test_logits_a_bit_apart(G, top, best):
+    """Neighbouring floats, some of them equal, in many clusters: the order is that of the floats, to the last bit."""
+    import torch
+    rng = np.random.default_rng(G + best)
+    E = 160
+    centre = rng.normal(size=(200, 12)).astype(np.float32) * 3
+    l = np.take_along_axis(centre, rng.integers(0, 12, (200, E)), 1)
+    l = (l.view(np.int32) + rng.integers(-3, 4, l.shape)).astype(np.int32).view(np.float32)
+    _compare(mbd.Router(E, 8, 0, True, G, top, best), torch.from_numpy(l).cuda())
 
 
 @pytest.mark.gpu

@@ -111,7 +111,7 @@ def _run(R, K, x="bf16", res="none", out="bf16", eight=False, gain=True, seed=0,
 
 
 SHAPES = [(1, 1), (1, 7), (3, 8), (5, 33), (2, 1001), (700, 64), (301, 1032), (4, 9216), (2, 32768), (1, 40008), (2, 32771), (600, 8192), (333, 24), (601, 1003),
-          (1300, 513), (310, 8200), (300, 16384), (297, 512), (2000, 8)]
+          (1300, 513), (310, 8200), (300, 16384), (297, 512), (2000, 8), (299, 12001), (320, 4104), (400, 2047)]
 
 
 @pytest.mark.gpu
@@ -181,6 +181,15 @@ def test_views_places_of_inputs_and_streams(K):
         _check(y, want, want.abs(), (_n(K) / 2 + 8) * U, torch.bfloat16)
         for c in (0, K + 1, 2 * K + 2, 3 * K + 3, 3 * K + 4):
             assert torch.equal(wide[:, c], before[:, c])
+        a, b = torch.randn(R, K, device="cuda", generator=gen), torch.randn(R, K, device="cuda", generator=gen)
+        held = a + b
+        z = torch.empty_like(b)
+        mbd.rms_norm(a, gain=gain, residual=b, h=a, y=b, eps=EPS)   # h on x, y on the residual
+        want, _ = _norm64(held, gain)
+        assert torch.equal(a, held)
+        _check(b, want, want.abs(), (_n(K) / 2 + 8) * U, torch.float32)
+        mbd.rms_norm(a, residual=a, h=z, eps=EPS, y=a)               # the same tensor twice
+        assert torch.equal(z, held + held)
         dense = x.contiguous()
         want, _ = _norm64(dense, None)
         mbd.rms_norm(dense, y=dense, eps=EPS)                      # y on x
