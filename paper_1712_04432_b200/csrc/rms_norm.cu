@@ -7,7 +7,7 @@
 //
 // Each tensor passes once: the row stays in registers between the sum and the result, the gain and the columns' sums of dg
 // in the registers of the threads that own the columns (blocks take row after row).  HBM bounds large calls, latency small ones.
-// Rows of whole vectors come through shared memory by asynchronous copies, each thread its own columns, STAGES rows ahead: a thread waits for
+// Where blocks keep something from row to row, rows come through shared memory by asynchronous copies some rows ahead: a warp waits for
 // its own copies only, and how much is under way does not depend on registers.
 #include <math_constants.h>
 
@@ -337,10 +337,79 @@ __global__ void __launch_bounds__(1024) rms_norm_few_kernel(const __grid_constan
   if (p.q && t == 0) p.scale[r] = c.s * inv;
 }
 
-// Many rows: one block per SM, blockDim.x / N rows at a time, each with NV vectors a thread.  RING: they come through shared memory,
-// p.stages rows deep.
-template <typename TX, typename TR, bool RES, int N, int NV, bool RING, bool WIDE>
-__global__ void __launch_bounds__(FORWARD_THREADS) rms_norm_kernel(const __grid_constant__ Norm p) {
+// More rows, N threads and NV vectors each, 128 threads a block at least: nothing is held from one row to the next, the rows of other blocks hide
+// the wait for a row.
+template <typename TX, typename TR, bool RES, int N, int NV, bool WIDE>
+__global__ void __launch_bounds__(N < 128 ? 128 : N) rms_norm_direct_kernel(const __grid_constant__ Norm p) {
+  __shared__ Exchange ex;
+  const int t = threadIdx.x & (N - 1);
+  const int64_t r = blockIdx.x * static_cast<int64_t>(blockDim.x / N) + threadIdx.x / N;
+  int turn = 0;
+  pdl_trigger();
+  pdl_wait();
+  if (r >= p.R) return;
+  Raw8<TX> x[NV];
+  Raw8<TR> res[NV], h[NV];
+  const TX* x_row = static_cast<const TX*>(p.x) + r * p.ldx;
+  const TR* res_row = static_cast<const TR*>(p.res) + r * p.ldres;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) load8<WIDE>(x_row, t, j, N, p.K, x[j]);
+  if (RES) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) load8<WIDE>(res_row, t, j, N, p.K, res[j]);
+  }
+  f32x2 sum2 = pair(0.f, 0.f);
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    h[j] = stream8<TX, TR, RES>(x[j], res[j]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum2 = fma2(h[j].two(i), h[j].two(i), sum2);
+  }
+  if (RES && p.h) {
+    TR* out = static_cast<TR*>(p.h) + r * p.ldh;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) store8<WIDE>(out, t, j, N, p.K, h[j]);
+  }
+  if (p.q) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      f32x2 g[4];
+      gain8<WIDE>(p.gain, t, j, N, p.K, g);
+      top = largest8(h[j], g, top);
+    }
+  }
+  float sum = both(sum2), none = 0.f;
+  over_row<false, true>(ex, turn, N, sum, none, top);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) h[j].repack();
+  const float inv_K = __fdiv_rn(1.f, static_cast<float>(p.K));
+  float inv = root(sum, inv_K, p.eps);
+  if (sum == CUDART_INF_F) {
+    sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const Raw8<TR> z = smaller8(h[j]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(z.at(i), z.at(i), sum);
+    }
+    uint32_t unused = 0;
+    over_row<false, false>(ex, turn, N, sum, none, unused);
+    inv = root(sum, inv_K, 0.f) * SMALLER;
+  }
+  Scale c{};
+  if (p.q) {
+    c = scale_of(top);
+    if (t == 0) p.scale[r] = c.s * inv;
+  }
+  results<NV, WIDE>(p, r, t, N, h, inv, c, [&](int j, f32x2* g) { gain8<WIDE>(p.gain, t, j, N, p.K, g); });
+}
+
+// Many rows with little traffic each (no residual, or results in 8 bits): one block per SM, blockDim.x / N rows at a time, which come through
+// shared memory, p.stages rows deep; the gain lies there too.
+template <typename TX, typename TR, bool RES, int N, int NV>
+__global__ void __launch_bounds__(FORWARD_THREADS) rms_norm_ring_kernel(const __grid_constant__ Norm p) {
+  constexpr bool WIDE = true;
   __shared__ Exchange ex;
   extern __shared__ __align__(16) char memory[];
   constexpr int X_BYTES = NV * 8 * static_cast<int>(sizeof(TX)) * N, STAGE = X_BYTES + (RES ? NV * 8 * static_cast<int>(sizeof(TR)) * N : 0);
@@ -351,11 +420,9 @@ __global__ void __launch_bounds__(FORWARD_THREADS) rms_norm_kernel(const __grid_
   const uint32_t ring_at = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
   const float inv_K = __fdiv_rn(1.f, static_cast<float>(p.K));
   int turn = 0;
-  if constexpr (RING) {
-    for (int s = 0; s < p.stages; ++s) {
-      clear_row<N, NV, WIDE, TX>(ring_at + s * STAGE, t, p.K);
-      if (RES) clear_row<N, NV, WIDE, TR>(ring_at + s * STAGE + X_BYTES, t, p.K);
-    }
+  for (int s = 0; s < p.stages; ++s) {
+    clear_row<N, NV, WIDE, TX>(ring_at + s * STAGE, t, p.K);
+    if (RES) clear_row<N, NV, WIDE, TR>(ring_at + s * STAGE + X_BYTES, t, p.K);
   }
   pdl_trigger();
   pdl_wait();
@@ -373,9 +440,7 @@ __global__ void __launch_bounds__(FORWARD_THREADS) rms_norm_kernel(const __grid_
     }
     copies_sent();
   };
-  if constexpr (RING) {
-    for (int s = 0; s < p.stages - 1; ++s) send(first + s * step, s);
-  }
+  for (int s = 0; s < p.stages - 1; ++s) send(first + s * step, s);
   keep_gain<N, NV, WIDE>(gain, p.gain, p.K);
   __syncthreads();
   int s = 0;
@@ -383,30 +448,19 @@ __global__ void __launch_bounds__(FORWARD_THREADS) rms_norm_kernel(const __grid_
     Raw8<TR> h[NV];
     f32x2 sum2 = pair(0.f, 0.f);
     uint32_t top = 0;
-    if constexpr (RING) {
-      __syncwarp();                                        // (the warp is done with the stage of the row before)
-      send(r + (p.stages - 1) * step, s == 0 ? p.stages - 1 : s - 1);
-      copies_landed(p.stages - 1);
-      __syncwarp();
-    }
+    __syncwarp();                                          // (the warp is done with the stage of the row before)
+    send(r + (p.stages - 1) * step, s == 0 ? p.stages - 1 : s - 1);
+    copies_landed(p.stages - 1);
+    __syncwarp();
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       Raw8<TX> x;
       Raw8<TR> res;
-      if constexpr (RING) {
-        take8<N, WIDE>(ring_at + s * STAGE, t, j, x);
-        if (RES) take8<N, WIDE>(ring_at + s * STAGE + X_BYTES, t, j, res);
-      } else {
-        load8<WIDE>(x_row, t, j, N, p.K, x);
-        if (RES) load8<WIDE>(res_row, t, j, N, p.K, res);
-      }
+      take8<N, WIDE>(ring_at + s * STAGE, t, j, x);
+      if (RES) take8<N, WIDE>(ring_at + s * STAGE + X_BYTES, t, j, res);
       h[j] = stream8<TX, TR, RES>(x, res);
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum2 = fma2(h[j].two(i), h[j].two(i), sum2);
-    }
-    if constexpr (!RING) {
-      x_row += x_step;
-      res_row += res_step;
     }
     if (RES && p.h) {
       TR* out = static_cast<TR*>(p.h) + r * p.ldh;
@@ -447,7 +501,7 @@ __global__ void __launch_bounds__(FORWARD_THREADS) rms_norm_kernel(const __grid_
     results<NV, WIDE>(p, r, t, N, h, inv, c, [&](int j, f32x2* g) { kept_gain<N, WIDE>(gain, t, j, g); });
     s = s == p.stages - 1 ? 0 : s + 1;
   }
-  if constexpr (RING) asm volatile("cp.async.wait_all;" ::: "memory");
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // A row too long for registers: read a second time.
@@ -895,35 +949,55 @@ template <auto KERNEL, typename P> cudaError_t launch_shape(P p, const Shape& s,
   return launch_pdl(KERNEL, dim3(static_cast<unsigned>(grid)), dim3(s.n * s.rows), bytes, stream, 1, p);
 }
 
-template <typename TX, typename TR, bool RES, bool RING, bool WIDE>
-cudaError_t launch_rows(const Norm& p, const Shape& s, int64_t grid, cudaStream_t stream) {
-  switch (s.nv * 1024 + s.n) {
-    case 2 * 1024 + 32: return launch_shape<rms_norm_kernel<TX, TR, RES, 32, 2, RING, WIDE>>(p, s, s.bytes, grid, stream);
-    case 2 * 1024 + 64: return launch_shape<rms_norm_kernel<TX, TR, RES, 64, 2, RING, WIDE>>(p, s, s.bytes, grid, stream);
-    case 2 * 1024 + 128: return launch_shape<rms_norm_kernel<TX, TR, RES, 128, 2, RING, WIDE>>(p, s, s.bytes, grid, stream);
-    case 2 * 1024 + 256: return launch_shape<rms_norm_kernel<TX, TR, RES, 256, 2, RING, WIDE>>(p, s, s.bytes, grid, stream);
-    case 4 * 1024 + 32: return launch_shape<rms_norm_kernel<TX, TR, RES, 32, 4, RING, WIDE>>(p, s, s.bytes, grid, stream);
-    case 4 * 1024 + 64: return launch_shape<rms_norm_kernel<TX, TR, RES, 64, 4, RING, WIDE>>(p, s, s.bytes, grid, stream);
-    case 4 * 1024 + 128: return launch_shape<rms_norm_kernel<TX, TR, RES, 128, 4, RING, WIDE>>(p, s, s.bytes, grid, stream);
-    case 4 * 1024 + 256: return launch_shape<rms_norm_kernel<TX, TR, RES, 256, 4, RING, WIDE>>(p, s, s.bytes, grid, stream);
-    default: return launch_shape<rms_norm_kernel<TX, TR, RES, 512, 4, RING, WIDE>>(p, s, s.bytes, grid, stream);
+// How rows of K values go directly: N threads and NV vectors.
+template <typename TX, typename TR, bool RES, bool WIDE>
+cudaError_t launch_direct(Norm p, cudaStream_t stream) {
+  const int nv = p.K <= 512 ? 2 : p.K <= 1024 ? 4 : p.K <= 4096 ? 2 : 4;      // (a warp to itself is worth more vectors; 8 warps are enough)
+  p.n = pow2_threads((p.K + 8 * nv - 1) / (8 * nv), 256);
+  const int threads = p.n < 128 ? 128 : p.n, rows = threads / p.n;
+  const dim3 grid(static_cast<unsigned>((p.R + rows - 1) / rows)), block(threads);
+  switch (nv * 1024 + p.n) {
+    case 2 * 1024 + 32: return launch_pdl(rms_norm_direct_kernel<TX, TR, RES, 32, 2, WIDE>, grid, block, 0, stream, 1, p);
+    case 2 * 1024 + 128: return launch_pdl(rms_norm_direct_kernel<TX, TR, RES, 128, 2, WIDE>, grid, block, 0, stream, 1, p);
+    case 2 * 1024 + 256: return launch_pdl(rms_norm_direct_kernel<TX, TR, RES, 256, 2, WIDE>, grid, block, 0, stream, 1, p);
+    case 4 * 1024 + 32: return launch_pdl(rms_norm_direct_kernel<TX, TR, RES, 32, 4, WIDE>, grid, block, 0, stream, 1, p);
+    default: return launch_pdl(rms_norm_direct_kernel<TX, TR, RES, 256, 4, WIDE>, grid, block, 0, stream, 1, p);
   }
 }
 
+template <typename TX, typename TR, bool RES>
+cudaError_t launch_ring(const Norm& p, const Shape& s, int sms, cudaStream_t stream) {
+  const int64_t want = (p.R + s.rows - 1) / s.rows, grid = want < sms ? want : sms;
+  switch (s.nv * 1024 + s.n) {
+    case 2 * 1024 + 32: return launch_shape<rms_norm_ring_kernel<TX, TR, RES, 32, 2>>(p, s, s.bytes, grid, stream);
+    case 4 * 1024 + 32: return launch_shape<rms_norm_ring_kernel<TX, TR, RES, 32, 4>>(p, s, s.bytes, grid, stream);
+    case 4 * 1024 + 64: return launch_shape<rms_norm_ring_kernel<TX, TR, RES, 64, 4>>(p, s, s.bytes, grid, stream);
+    case 4 * 1024 + 128: return launch_shape<rms_norm_ring_kernel<TX, TR, RES, 128, 4>>(p, s, s.bytes, grid, stream);
+    case 4 * 1024 + 256: return launch_shape<rms_norm_ring_kernel<TX, TR, RES, 256, 4>>(p, s, s.bytes, grid, stream);
+    default: return launch_shape<rms_norm_ring_kernel<TX, TR, RES, 512, 4>>(p, s, s.bytes, grid, stream);
+  }
+}
+
+// Few rows go one per block, for the latency.  Others go directly where their traffic hides what a row costs besides (8 bytes a value: 8192 x
+// 4096 bf16 with residual 43 us, by the ring 48; 8192 x 2048 floats with one 42, 48), or where they are too few to fill the ring (2000 x 4096 without
+// a residual 9.4 us, 10.4; 1000 x 1024 with one 2.5, 4.6); through the ring where there is less traffic (8192 x 4096 bf16 without a residual 25 us,
+// directly 32; in 8 bits with one 43, 48).
 template <typename TX, typename TR, bool RES, bool WIDE>
 cudaError_t launch_norm(Norm p, int sms, cudaStream_t stream) {
-  constexpr bool RING = WIDE || (sizeof(TX) == 4 && (!RES || sizeof(TR) == 4));
-  if (p.K <= 8192 && p.R < 2 * sms) {        // few rows: a vector a thread, for the latency
-    p.n = pow2_threads((p.K + 7) / 8, 1024);
-    return launch_pdl(rms_norm_few_kernel<TX, TR, RES, WIDE>, dim3(static_cast<unsigned>(p.R)), dim3(p.n), 0, stream, 1, p);
+  if (p.K <= 8192) {
+    if (p.R < 2 * sms) {
+      p.n = pow2_threads((p.K + 7) / 8, 1024);
+      return launch_pdl(rms_norm_few_kernel<TX, TR, RES, WIDE>, dim3(static_cast<unsigned>(p.R)), dim3(p.n), 0, stream, 1, p);
+    }
+    const int bytes = static_cast<int>(sizeof(TX) + (RES ? (p.h ? 2 : 1) * sizeof(TR) : 0)) + (p.y ? (p.y_bf16 ? 2 : 4) : 0);
+    if (!WIDE || (bytes >= 8 && !p.q) || p.R * p.K <= 10000000) return launch_direct<TX, TR, RES, WIDE>(p, stream);
   }
-  const Shape s = shape_of(p.K, 8 * static_cast<int>(sizeof(TX) + (RES ? sizeof(TR) : 0)), RING, FORWARD_THREADS, 512);
-  if (p.K > LONGEST || (RING && !s.stages)) {
-    p.n = 1024;
-    return launch_pdl(rms_norm_long_kernel<TX, TR, RES, WIDE>, dim3(static_cast<unsigned>(p.R)), dim3(1024), 0, stream, 1, p);
+  if constexpr (WIDE) {
+    const Shape s = shape_of(p.K, 8 * static_cast<int>(sizeof(TX) + (RES ? sizeof(TR) : 0)), true, FORWARD_THREADS, 512);
+    if (p.K <= LONGEST && s.stages) return launch_ring<TX, TR, RES>(p, s, sms, stream);
   }
-  const int64_t want = (p.R + s.rows - 1) / s.rows;
-  return launch_rows<TX, TR, RES, RING, WIDE>(p, s, want < sms ? want : sms, stream);
+  p.n = 1024;
+  return launch_pdl(rms_norm_long_kernel<TX, TR, RES, WIDE>, dim3(static_cast<unsigned>(p.R)), dim3(1024), 0, stream, 1, p);
 }
 
 template <typename TD, typename TH, bool RING, bool WIDE>
