@@ -278,13 +278,15 @@ __device__ __forceinline__ void results(const Norm& p, int64_t r, int t, int n, 
     }
   }
 }
-template <typename TR> __device__ __forceinline__ uint32_t largest8(const Raw8<TR>& h, const f32x2* g, uint32_t top) {
+// The largest |h g| so far, by its bits (their order is that of the magnitudes, infinities and NaN last).
+template <typename TR> __device__ __forceinline__ uint32_t largest8(const Raw8<TR>& h, const f32x2* g, uint32_t so_far) {
+  float top = __uint_as_float(so_far);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 u = floats(mul2(h.two(i), g[i]));
-    top = max(top, max(__float_as_uint(u.x) & 0x7FFFFFFFu, __float_as_uint(u.y) & 0x7FFFFFFFu));
+    asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(u.x), "f"(u.y));
   }
-  return top;
+  return __float_as_uint(top) & 0x7FFFFFFFu;
 }
 template <typename TR> __device__ __forceinline__ Raw8<TR> smaller8(const Raw8<TR>& h) {
   float v[8];
