@@ -99,15 +99,14 @@ __device__ __forceinline__ float sigmoid_small(float z) {      // min(sigmoid(z)
   return t * r;
 }
 
-// Which of the groups stay: lane l has the score of group l >> shift; equal ones by rising index.
-template <typename C> __device__ __forceinline__ bool among_best(C mine, int shift, int top_groups, int lane) {
-  bool keep = false;
-  for (int j = 0; j < top_groups; ++j) {
-    const C left = keep ? 0 : mine, first = largest(left);
-    if (!first) break;
-    if ((__ffs(__ballot_sync(0xffffffffu, left == first)) - 1) >> shift == lane >> shift) keep = true;
+// Whether a group is among the best: lane l has the score of group l >> shift; equal ones by rising index.
+template <typename C> __device__ __forceinline__ bool among_best(C mine, int shift, int groups, int top_groups, int lane) {
+  int rank = 0;
+  for (int g = 0; g < groups; ++g) {
+    const C other = __shfl_sync(0xffffffffu, mine, g << shift);
+    rank += other > mine || (other == mine && g < lane >> shift);
   }
-  return keep;
+  return mine && rank < top_groups;                            // (lanes behind the last group have 0)
 }
 
 // Scores in double, for what lies too near to each other for floats.  One exponential and one quotient for both kinds: this code is met
@@ -172,7 +171,7 @@ __device__ __noinline__ int choose_exactly(const Route& p, const T* row, const f
       }
       if (lane == g) mine = of;
     }
-    const unsigned kept = __ballot_sync(0xffffffffu, among_best(mine, 0, p.top_groups, lane));
+    const unsigned kept = __ballot_sync(0xffffffffu, among_best(mine, 0, p.G, p.top_groups, lane));
 #pragma unroll 1
     for (int i = 0; i < per; ++i)
       if (first_e + i < p.E && !(kept >> (first_e + i) / S & 1u)) key[i] = 0;
@@ -273,9 +272,10 @@ template <int N> __device__ __forceinline__ void sort_falling(uint32_t (&s)[N]) 
 // softmax needs them.
 struct Choice { int id; float z, top, total; bool unsure; };          // z: the logit of expert id
 
-// Keys with a bias: fixed if all biases are within 0.99, (score + bias + 1) 2^30, the biases' share in shared memory; else the float sum's code.
+// list: k words of the warp's in shared memory.  Keys with a bias: fixed if all biases are within 0.99, (score + bias + 1) 2^30, the biases' share in shared memory; else the float sum's code.
 template <int NPL, typename T>
-__device__ __forceinline__ Choice choose(const Route& p, const T* row, const float (&l)[NPL], const float* bias, const uint32_t* bias_steps, bool fixed, int lane) {
+__device__ __forceinline__ Choice choose(const Route& p, const T* row, const float (&l)[NPL], const float* bias, const uint32_t* bias_steps, bool fixed, uint2* list,
+                                        int lane) {
   constexpr uint32_t LOW = NPL - 1;
   const bool by_two = p.G > 1 && p.best == 2, scored = p.bias || by_two;      // whether the choice needs more than the order of the logits
   Choice c{-1, 0.f, -CUDART_INF_F, 1.f, false};
@@ -291,17 +291,25 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
   }
   const float inv_total = p.sigmoid ? 1.f : __fdividef(1.f, c.total);
   auto small = [&](float z) { return p.sigmoid ? sigmoid_small(z) : expf(z - c.top) * inv_total; };
-  auto steps = [&](float z) { return z != z || inv_total != inv_total ? NAN_CODE : (1u << 30) + steps_of(small(z), p.sigmoid && z >= 0.f); };
+  auto steps = [&](float z, bool by_sigmoid) {                 // one in front
+    const float s = by_sigmoid ? sigmoid_small(z) : expf(z - c.top) * inv_total;
+    return s != s ? NAN_CODE : (1u << 30) + steps_of(s, by_sigmoid && z >= 0.f);
+  };
+  auto in_steps = [&](float z, uint32_t bias, bool by_sigmoid) {
+    const uint32_t s = steps(z, by_sigmoid);
+    return z == -CUDART_INF_F ? 0u : s == NAN_CODE ? s : s + bias;
+  };
   uint32_t key[NPL];
   if (p.bias && fixed) {
+    if (p.sigmoid) {
 #pragma unroll
-    for (int i = 0; i < NPL; ++i) {
-      key[i] = 0;
-      if (l[i] != -CUDART_INF_F) {                             // (so the expert exists)
-        const uint32_t s = steps(l[i]);
-        key[i] = ((s == NAN_CODE ? s : s + bias_steps[lane * NPL + i]) & ~LOW) | (LOW - i);
-      }
+      for (int i = 0; i < NPL; ++i) key[i] = in_steps(l[i], bias_steps[lane * NPL + i], true);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NPL; ++i) key[i] = in_steps(l[i], bias_steps[lane * NPL + i], false);
     }
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) key[i] = key[i] ? (key[i] & ~LOW) | (LOW - i) : 0u;
   } else if (p.bias) {
 #pragma unroll
     for (int i = 0; i < NPL; ++i) {
@@ -323,7 +331,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
   if (p.G > 1) {
     const bool by_score = by_two && !p.bias, sums = by_two && (fixed || by_score);
     // a lane's two best of a group, as the group counts them
-    auto counted = [&](uint32_t k) { return by_score && k ? steps(logit(row, lane * NPL + static_cast<int>(LOW - (k & LOW)))) : k & ~LOW; };
+    auto counted = [&](uint32_t k) { return by_score && k ? steps(logit(row, lane * NPL + static_cast<int>(LOW - (k & LOW))), p.sigmoid) : k & ~LOW; };
     auto group_score = [&](uint32_t first, uint32_t second) {
       if (p.best == 1 || !first) return first;
       if (first <= 2 * NAN_CODE || (second && second <= 2 * NAN_CODE)) return NAN_CODE;
@@ -340,7 +348,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
         a = max(a, a2);
       }
       mine = group_score(a, b);
-      keep = among_best(mine, p.group_lanes - 1, p.top_groups, lane);
+      keep = among_best(mine, p.group_lanes - 1, p.G, p.top_groups, lane);
       if (!keep) {
 #pragma unroll
         for (int i = 0; i < NPL; ++i) key[i] = 0;
@@ -361,7 +369,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
         const uint32_t second = largest(lane == __ffs(owners) - 1 ? b : a);
         if (lane == g) mine = group_score(first, second);
       }
-      keep = among_best(mine, 0, p.top_groups, lane);          // (lanes behind the last group have 0)
+      keep = among_best(mine, 0, p.G, p.top_groups, lane);
       const unsigned kept = __ballot_sync(0xffffffffu, keep);
 #pragma unroll
       for (int i = 0; i < NPL; ++i) {
@@ -382,41 +390,33 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
       }
     }
   }
-  uint32_t mine = 0;
-  int chosen = 0;
   for (int j = 0; j < p.k; ++j) {
     const uint32_t own = key[0] & ~LOW, first = largest(own);
-    if (!first) break;
-    const int src = __ffs(__ballot_sync(0xffffffffu, own == first)) - 1;
-    const uint32_t got = __shfl_sync(0xffffffffu, key[0], src);
-    if (lane == j) {
-      mine = first;
-      c.id = src * NPL + static_cast<int>(LOW - (got & LOW));
-    }
-    if (lane == src) {
+    if (lane == __ffs(__ballot_sync(0xffffffffu, own == first)) - 1) {
+      list[j] = make_uint2(first, first ? lane * NPL + (LOW - (key[0] & LOW)) : ~0u);
 #pragma unroll
       for (int i = 0; i + 1 < NPL; ++i) key[i] = key[i + 1];
       key[NPL - 1] = 0;
     }
-    chosen = j + 1;
   }
+  __syncwarp();
+  const uint2 got = lane < p.k ? list[lane] : make_uint2(0u, ~0u);
+  const uint32_t mine = got.x;
+  const int chosen = __popc(__ballot_sync(0xffffffffu, mine != 0));
+  c.id = static_cast<int>(got.y);
   if (c.id >= 0) c.z = logit(row, c.id);
   if (!p.bias && sizeof(T) == 2) return c;                     // (logits of bf16 end in zeros: nothing was given away)
   if (c.unsure) return c;
   // Neighbours in the order, and the last one against those that are left; equal logits with equal biases are really equal.  A first look by
   // the largest error there can be, a second one by the two experts' own small parts.
-  const float value = p.bias && !fixed ? value_of(mine) : 0.f;
   const uint32_t reach = p.bias && fixed ? static_cast<uint32_t>(coarse * STEPS) + NPL + 4 : 0u;
-  const float reach_value = coarse + (NPL + 2) * 1.2e-7f * fabsf(value);
-  auto close = [&](uint32_t hi, uint32_t lo, float value_hi, float within) {
-    if (hi <= 2 * NAN_CODE || lo <= 2 * NAN_CODE) return true;
-    return p.bias && !fixed ? !(value_hi - value_of(lo) > within) : hi - lo <= reach;
+  auto close = [&](uint32_t hi, uint32_t lo) {
+    if (!p.bias || fixed) return hi - lo <= reach || lo <= 2 * NAN_CODE;
+    const float v = value_of(hi);
+    return !(v - value_of(lo) > coarse + (NPL + 2) * 1.2e-7f * fabsf(v));
   };
-  const uint32_t next = __shfl_down_sync(0xffffffffu, mine, 1);
-  const uint32_t last = __shfl_sync(0xffffffffu, mine, p.k - 1), left = key[0] & ~LOW;
-  const float value_last = __shfl_sync(0xffffffffu, value, p.k - 1), reach_last = __shfl_sync(0xffffffffu, reach_value, p.k - 1);
-  const bool near_next = lane + 1 < chosen && close(mine, next, value, reach_value);
-  const bool near_left = chosen == p.k && left && close(last, left, value_last, reach_last);
+  const uint32_t next = __shfl_down_sync(0xffffffffu, mine, 1), last = __shfl_sync(0xffffffffu, mine, p.k - 1), left = key[0] & ~LOW;
+  const bool near_next = lane + 1 < chosen && close(mine, next), near_left = chosen == p.k && left && close(last, left);
   if (__any_sync(0xffffffffu, near_next || near_left)) {
     const float z = c.z, b = c.id >= 0 && p.bias ? bias[c.id] : 0.f, s = p.bias && fixed && c.id >= 0 ? small(z) : 0.f;
     auto differ = [&](uint32_t hi, uint32_t lo, float z1, float b1, float s1, float z2, float b2, float s2) {
@@ -432,7 +432,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
 #pragma unroll
       for (int i = 0; i < NPL; ++i) {
         const int e = lane * NPL + static_cast<int>(LOW - (key[i] & LOW));
-        const bool may = key[i] && close(last, key[i] & ~LOW, value_last, reach_last);
+        const bool may = key[i] && close(last, key[i] & ~LOW);
         if (may) {
           const float ze = logit(row, e);
           near |= differ(last, key[i] & ~LOW, zk, bk, sk, ze, p.bias ? bias[e] : 0.f, p.bias && fixed ? small(ze) : 0.f);
@@ -460,8 +460,9 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
 // chosen one, so that scores below float's range keep their ratios: sigmoid(z) is exp(z) far below zero.
 __device__ __forceinline__ float share(float z, bool there, bool by_sigmoid, bool renorm, float top, float total) {
   if (!renorm) return there ? (by_sigmoid ? sigmoid(z) : __fdividef(expf(z - top), total)) : 0.f;
-  const float most = warp_max(there ? z : -CUDART_INF_F);
-  const float r = !there || z == -CUDART_INF_F ? 0.f : by_sigmoid && !(most < -60.f) ? sigmoid(z) : expf(z - most);
+  const bool tiny = by_sigmoid && !__any_sync(0xffffffffu, there && z >= -60.f);
+  const float most = !by_sigmoid || tiny ? warp_max(there ? z : -CUDART_INF_F) : 0.f;
+  const float r = !there || z == -CUDART_INF_F ? 0.f : by_sigmoid && !tiny ? sigmoid(z) : expf(z - most);
   const float sum = warp_sum(r);
   return there && sum != 0.f ? __fdividef(r, sum) : 0.f;
 }
@@ -493,6 +494,7 @@ __global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Rou
   __shared__ uint32_t chose[MAX_E][SUB / 32];
   __shared__ int running[MAX_E + 1];
   __shared__ int16_t ids[SUB * MAX_K];
+  __shared__ uint2 lists[32][MAX_K];
   __shared__ __align__(16) float bias[MAX_E];
   __shared__ __align__(16) uint32_t bias_steps[MAX_E];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -528,7 +530,7 @@ __global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Rou
       else if (i + warps < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (t + warps) * p.ld, p.E, p.whole, lane, next);
       if (t < live) {
         const T* row = static_cast<const T*>(p.logits) + t * p.ld;
-        const Choice c = choose<NPL>(p, row, l, bias, bias_steps, fixed, lane);
+        const Choice c = choose<NPL>(p, row, l, bias, bias_steps, fixed, lists[warp], lane);
         float z = c.z;
         id = c.id;
         if (c.unsure) {
