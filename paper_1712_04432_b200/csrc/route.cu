@@ -41,7 +41,7 @@ struct Route {
   int whole;                    // rows of logits can be read in whole runs of a lane's experts
   int sigmoid, renorm, G, top_groups, best;
   uint32_t by_group;            // e / (E / G) = e * by_group >> 20
-  int group_lanes;              // where every lane has experts of one group: 1 + log2 of the lanes of a group; else 0
+  int S, group_lanes, per;      // S: E / G; groups dealt out to lanes: 1 + log2 of the lanes of a group, and the experts of a lane; else 0
   float scale;
 };
 
@@ -150,7 +150,7 @@ __device__ __noinline__ int choose_exactly(const Route& p, const T* row, const f
     count[i] = by_score ? code_of(s) : key[i];
   }
   if (p.G > 1) {
-    const int S = p.E / p.G;
+    const int S = p.S;
     code64 mine = 0;                                           // lane g: the score of group g
 #pragma unroll 1
     for (int g = 0; g < p.G; ++g) {
@@ -216,12 +216,11 @@ __device__ __noinline__ int settle(const Route& p, const T* row, const float* bi
   return got;
 }
 
-// NPL logits of lane `lane`, experts lane * NPL on; -inf behind the last.
+// NPL logits of a lane, experts `first` on; -inf behind its `count`.
 template <int NPL, typename T>
-__device__ __forceinline__ void logits_of(const T* row, int E, bool whole, int lane, float (&l)[NPL]) {
-  const int first = lane * NPL;
+__device__ __forceinline__ void logits_of(const T* row, int first, int count, bool whole, float (&l)[NPL]) {
   if (NPL * sizeof(T) >= 4 && whole) {                         // whole runs of NPL, aligned
-    if (first >= E) {
+    if (count == 0) {
 #pragma unroll
       for (int i = 0; i < NPL; ++i) l[i] = -CUDART_INF_F;
       return;
@@ -246,7 +245,7 @@ __device__ __forceinline__ void logits_of(const T* row, int E, bool whole, int l
       l[i] = __uint_as_float(sizeof(T) == 4 ? w[i] : i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
   } else {
 #pragma unroll
-    for (int i = 0; i < NPL; ++i) l[i] = first + i < E ? logit(row, first + i) : -CUDART_INF_F;
+    for (int i = 0; i < NPL; ++i) l[i] = i < count ? logit(row, first + i) : -CUDART_INF_F;
   }
 }
 
@@ -272,10 +271,10 @@ template <int N> __device__ __forceinline__ void sort_falling(uint32_t (&s)[N]) 
 // softmax needs them.
 struct Choice { int id; float z, top, total; bool unsure; };          // z: the logit of expert id
 
-// list: k words of the warp's in shared memory.  Keys with a bias: fixed if all biases are within 0.99, (score + bias + 1) 2^30, the biases' share in shared memory; else the float sum's code.
+// first_e: the lane's first expert.  list: k words of the warp's in shared memory.  Keys with a bias: fixed if all biases are within 0.99, (score + bias + 1) 2^30, the biases' share in shared memory; else the float sum's code.
 template <int NPL, typename T>
 __device__ __forceinline__ Choice choose(const Route& p, const T* row, const float (&l)[NPL], const float* bias, const uint32_t* bias_steps, bool fixed, uint2* list,
-                                        int lane) {
+                                        int first_e, int lane) {
   constexpr uint32_t LOW = NPL - 1;
   const bool by_two = p.G > 1 && p.best == 2, scored = p.bias || by_two;      // whether the choice needs more than the order of the logits
   Choice c{-1, 0.f, -CUDART_INF_F, 1.f, false};
@@ -303,10 +302,10 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
   if (p.bias && fixed) {
     if (p.sigmoid) {
 #pragma unroll
-      for (int i = 0; i < NPL; ++i) key[i] = in_steps(l[i], bias_steps[lane * NPL + i], true);
+      for (int i = 0; i < NPL; ++i) key[i] = in_steps(l[i], bias_steps[first_e + i], true);
     } else {
 #pragma unroll
-      for (int i = 0; i < NPL; ++i) key[i] = in_steps(l[i], bias_steps[lane * NPL + i], false);
+      for (int i = 0; i < NPL; ++i) key[i] = in_steps(l[i], bias_steps[first_e + i], false);
     }
 #pragma unroll
     for (int i = 0; i < NPL; ++i) key[i] = key[i] ? (key[i] & ~LOW) | (LOW - i) : 0u;
@@ -315,7 +314,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
     for (int i = 0; i < NPL; ++i) {
       key[i] = 0;
       if (l[i] != -CUDART_INF_F) {
-        const float s = small(l[i]), v = (p.sigmoid && l[i] >= 0.f ? 1.f - s : s) + bias[lane * NPL + i];
+        const float s = small(l[i]), v = (p.sigmoid && l[i] >= 0.f ? 1.f - s : s) + bias[first_e + i];
         if (v != -CUDART_INF_F) key[i] = (code_of(v) & ~LOW) | (LOW - i);
       }
     }
@@ -331,7 +330,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
   if (p.G > 1) {
     const bool by_score = by_two && !p.bias, sums = by_two && (fixed || by_score);
     // a lane's two best of a group, as the group counts them
-    auto counted = [&](uint32_t k) { return by_score && k ? steps(logit(row, lane * NPL + static_cast<int>(LOW - (k & LOW))), p.sigmoid) : k & ~LOW; };
+    auto counted = [&](uint32_t k) { return by_score && k ? steps(logit(row, first_e + static_cast<int>(LOW - (k & LOW))), p.sigmoid) : k & ~LOW; };
     auto group_score = [&](uint32_t first, uint32_t second) {
       if (p.best == 1 || !first) return first;
       if (first <= 2 * NAN_CODE || (second && second <= 2 * NAN_CODE)) return NAN_CODE;
@@ -359,7 +358,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
         uint32_t a = 0, b = 0;
 #pragma unroll
         for (int i = 0; i < NPL; ++i) {
-          const int e = lane * NPL + static_cast<int>(LOW - (key[i] & LOW));
+          const int e = first_e + static_cast<int>(LOW - (key[i] & LOW));
           if (key[i] == 0 || static_cast<int>(e * p.by_group >> 20) != g) continue;
           const uint32_t v = counted(key[i]);
           if (v > a) { b = a; a = v; }
@@ -373,7 +372,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
       const unsigned kept = __ballot_sync(0xffffffffu, keep);
 #pragma unroll
       for (int i = 0; i < NPL; ++i) {
-        const int e = lane * NPL + static_cast<int>(LOW - (key[i] & LOW));
+        const int e = first_e + static_cast<int>(LOW - (key[i] & LOW));
         if (!(kept >> (e * p.by_group >> 20 & 31u) & 1u)) key[i] = 0;
       }
       sort_falling(key);
@@ -393,7 +392,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
   for (int j = 0; j < p.k; ++j) {
     const uint32_t own = key[0] & ~LOW, first = largest(own);
     if (lane == __ffs(__ballot_sync(0xffffffffu, own == first)) - 1) {
-      list[j] = make_uint2(first, first ? lane * NPL + (LOW - (key[0] & LOW)) : ~0u);
+      list[j] = make_uint2(first, first ? first_e + (LOW - (key[0] & LOW)) : ~0u);
 #pragma unroll
       for (int i = 0; i + 1 < NPL; ++i) key[i] = key[i + 1];
       key[NPL - 1] = 0;
@@ -431,7 +430,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
       const float zk = __shfl_sync(0xffffffffu, z, p.k - 1), bk = __shfl_sync(0xffffffffu, b, p.k - 1), sk = __shfl_sync(0xffffffffu, s, p.k - 1);
 #pragma unroll
       for (int i = 0; i < NPL; ++i) {
-        const int e = lane * NPL + static_cast<int>(LOW - (key[i] & LOW));
+        const int e = first_e + static_cast<int>(LOW - (key[i] & LOW));
         const bool may = key[i] && close(last, key[i] & ~LOW);
         if (may) {
           const float ze = logit(row, e);
@@ -495,11 +494,18 @@ __global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Rou
   __shared__ int running[MAX_E + 1];
   __shared__ int16_t ids[SUB * MAX_K];
   __shared__ uint2 lists[32][MAX_K];
-  __shared__ __align__(16) float bias[MAX_E];
-  __shared__ __align__(16) uint32_t bias_steps[MAX_E];
+  __shared__ __align__(16) float bias[MAX_E + 16];               // (a lane with fewer experts than places looks behind its last)
+  __shared__ __align__(16) uint32_t bias_steps[MAX_E + 16];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   pdl_trigger();
   pdl_wait();
+  // this lane's experts, those of one group where groups are dealt out to lanes
+  int first_e = lane * NPL, count = min(max(p.E - first_e, 0), NPL);
+  if (p.group_lanes) {
+    const int g = lane >> (p.group_lanes - 1), q = (lane & ((1 << (p.group_lanes - 1)) - 1)) * p.per;
+    first_e = g < p.G ? g * p.S + min(q, p.S) : 0;
+    count = g < p.G ? min(max(p.S - q, 0), p.per) : 0;
+  }
   const int live = p.count ? min(max(*p.count, 0), p.T) : p.T;
   int fits = 1;
   for (int e = threadIdx.x; e <= p.E; e += blockDim.x) {
@@ -519,18 +525,18 @@ __global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Rou
     const int tokens = static_cast<int>(min(end - sub, static_cast<int64_t>(SUB)));
     constexpr bool AHEAD = NPL < 16;                           // (with 16 more registers a thread 512 threads fit, not 1024: 16384 tokens of 512 experts 107 instead of 99 us)
     float next[NPL];                                           // the warp's next token is on its way
-    if (AHEAD && warp < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (sub + warp) * p.ld, p.E, p.whole, lane, next);
+    if (AHEAD && warp < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (sub + warp) * p.ld, first_e, count, p.whole, next);
     for (int i = warp; i < tokens; i += warps) {
       const int64_t t = sub + i;
       int id = -1;
       float w = 0.f, l[NPL];
 #pragma unroll
       for (int m = 0; m < NPL; ++m) l[m] = AHEAD ? next[m] : 0.f;
-      if (!AHEAD) logits_of<NPL>(static_cast<const T*>(p.logits) + t * p.ld, p.E, p.whole, lane, l);
-      else if (i + warps < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (t + warps) * p.ld, p.E, p.whole, lane, next);
+      if (!AHEAD) logits_of<NPL>(static_cast<const T*>(p.logits) + t * p.ld, first_e, count, p.whole, l);
+      else if (i + warps < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (t + warps) * p.ld, first_e, count, p.whole, next);
       if (t < live) {
         const T* row = static_cast<const T*>(p.logits) + t * p.ld;
-        const Choice c = choose<NPL>(p, row, l, bias, bias_steps, fixed, lists[warp], lane);
+        const Choice c = choose<NPL>(p, row, l, bias, bias_steps, fixed, lists[warp], first_e, lane);
         float z = c.z;
         id = c.id;
         if (c.unsure) {
@@ -716,17 +722,24 @@ int64_t blocks_of(int64_t T) { return T <= SUB ? 1 : (T + chunk_of(T) - 1) / chu
 
 template <typename T, int NPL> cudaError_t launch_npl(Route p, dim3 grid, dim3 block, cudaStream_t stream) {
   constexpr uint64_t BYTES = NPL * sizeof(T) < 16 ? NPL * sizeof(T) : 16;
-  p.whole = p.E % NPL == 0 && reinterpret_cast<uintptr_t>(p.logits) % BYTES == 0 && (p.T <= 1 || static_cast<uint64_t>(p.ld) * sizeof(T) % BYTES == 0);
-  const int S = p.E / p.G, lanes = S / NPL;
-  if (p.G > 1 && S % NPL == 0 && (lanes & (lanes - 1)) == 0)
-    for (p.group_lanes = 1; 1 << (p.group_lanes - 1) < lanes; ++p.group_lanes) {}
+  p.whole = p.E % NPL == 0 && (!p.group_lanes || (p.per == NPL && p.S % NPL == 0)) && reinterpret_cast<uintptr_t>(p.logits) % BYTES == 0 && (p.T <= 1 || static_cast<uint64_t>(p.ld) * sizeof(T) % BYTES == 0);
   return launch_pdl(route_kernel<T, NPL>, grid, block, 0, stream, 1, p);
 }
-template <typename T> cudaError_t launch(const Route& p, dim3 grid, dim3 block, cudaStream_t stream) {
-  if (p.E <= 32) return launch_npl<T, 1>(p, grid, block, stream);
-  if (p.E <= 64) return launch_npl<T, 2>(p, grid, block, stream);
-  if (p.E <= 128) return launch_npl<T, 4>(p, grid, block, stream);
-  if (p.E <= 256) return launch_npl<T, 8>(p, grid, block, stream);
+template <typename T> cudaError_t launch(Route p, dim3 grid, dim3 block, cudaStream_t stream) {
+  int per = (p.E + 31) / 32;
+  if (p.G > 1) {                                               // 1, 2, 4 .. lanes a group, if its experts find room in them
+    int log_lanes = 0;
+    while (p.G << (log_lanes + 1) <= 32) ++log_lanes;
+    const int of_lane = (p.S + (1 << log_lanes) - 1) >> log_lanes;
+    if (of_lane <= 16) {
+      p.group_lanes = 1 + log_lanes;
+      p.per = per = of_lane;
+    }
+  }
+  if (per <= 1) return launch_npl<T, 1>(p, grid, block, stream);
+  if (per <= 2) return launch_npl<T, 2>(p, grid, block, stream);
+  if (per <= 4) return launch_npl<T, 4>(p, grid, block, stream);
+  if (per <= 8) return launch_npl<T, 8>(p, grid, block, stream);
   return launch_npl<T, 16>(p, grid, block, stream);
 }
 
@@ -784,7 +797,7 @@ extern "C" mbd_status mbd_expert_route(const mbd_router* router, int64_t T, cons
   const bool one = T <= SUB;
   const Route p{logits_dev, bias_dev, count_dev, ids_dev, places_dev, offsets_dev, weights_dev, one ? nullptr : reinterpret_cast<uint16_t*>(scratch_dev), ld,
                 static_cast<int>(T), E, (E + 7) / 8 * 8, k, one ? SUB : chunk_of(T), 0, router->score == MBD_ROUTE_SIGMOID, router->renormalise != 0,
-                router->groups, router->top_groups, router->group_best, ((1u << 20) + S - 1) / S, 0, router->scale};
+                router->groups, router->top_groups, router->group_best, ((1u << 20) + S - 1) / S, static_cast<int>(S), 0, 0, router->scale};
   int warps = (E + 31) / 32;                                  // (a thread per expert at least)
   while (warps < (one ? T : chunk_of(T)) && warps < 32) ++warps;
   const dim3 grid(static_cast<unsigned>(blocks_of(T))), block(32 * warps);
