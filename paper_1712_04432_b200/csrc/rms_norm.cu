@@ -82,8 +82,8 @@ __device__ __forceinline__ void copies_landed(int ahead) {            // all but
 constexpr int MOST_STAGES = 4;
 constexpr int FORWARD_THREADS = 768, BACKWARD_THREADS = 512;   // of a block that takes many rows
 
-// Eight floats are two pieces of 16 bytes side by side: a thread that copied both would ask for each 32-byte sector twice (float rows at 3.7 instead
-// of 5 TB/s), so the lanes of a warp copy the warp's 1024 bytes in order and read the pieces that others brought; every second
+// Eight floats are two pieces of 16 bytes side by side: a thread that copied both would ask for each 32-byte sector twice (8192 x 2048 floats backward
+// 73 instead of 48 us), so the lanes of a warp copy the warp's 1024 bytes in order and read the pieces that others brought; every second
 // group of eight pieces is swapped in pairs, which keeps the reads apart in the banks.
 __device__ __forceinline__ uint32_t piece_at(int p) { return (p ^ (p >> 3 & 1)) * 16; }
 
@@ -297,7 +297,7 @@ template <typename TR> __device__ __forceinline__ Raw8<TR> smaller8(const Raw8<T
   return r;
 }
 
-// A few rows: one per block, a vector a thread.
+// A few rows: one per block, a vector a thread (16 x 1024 bf16 to 8 bits, with residual: 2.0 us, one round trip and a barrier).
 template <typename TX, typename TR, bool RES, bool WIDE>
 __global__ void __launch_bounds__(1024) rms_norm_few_kernel(const __grid_constant__ Norm p) {
   __shared__ Exchange ex;
@@ -340,7 +340,8 @@ __global__ void __launch_bounds__(1024) rms_norm_few_kernel(const __grid_constan
 }
 
 // More rows, N threads and NV vectors each, 128 threads a block at least: nothing is held from one row to the next, the rows of other blocks hide
-// the wait for a row.
+// the wait for a row.  HBM bounds it (8192 x 4096 bf16 with residual 43 us, 6.2 TB/s; torch copies
+// such tensors at 6.0 and adds them at 6.7).
 template <typename TX, typename TR, bool RES, int N, int NV, bool WIDE>
 __global__ void __launch_bounds__(N < 128 ? 128 : N) rms_norm_direct_kernel(const __grid_constant__ Norm p) {
   __shared__ Exchange ex;
@@ -408,7 +409,7 @@ __global__ void __launch_bounds__(N < 128 ? 128 : N) rms_norm_direct_kernel(cons
 }
 
 // Many rows with little traffic each (no residual, or results in 8 bits): one block per SM, blockDim.x / N rows at a time, which come through
-// shared memory, p.stages rows deep; the gain lies there too.
+// shared memory, p.stages rows deep; the gain lies there too.  8192 x 4096 bf16 25 us (5.4 TB/s), in 8 bits 33 us: instructions bound that one.
 template <typename TX, typename TR, bool RES, int N, int NV>
 __global__ void __launch_bounds__(FORWARD_THREADS) rms_norm_ring_kernel(const __grid_constant__ Norm p) {
   constexpr bool WIDE = true;
@@ -577,6 +578,10 @@ struct Grad {
   int K, n, stages, acc_shared;         // acc_shared (long rows): the block's sums lie in shared memory
 };
 
+// One block per SM, blockDim.x / N rows at a time through shared memory (RING; floats of any alignment too, bf16 in whole vectors); a row is read
+// from there twice, so that registers hold the sums of dg and little else.  8192 x 4096 bf16 with d_residual: 44 us (6.1 TB/s) without d_gain, 49
+// with it: the kernel below cannot start before the last block ends.  Two vectors a thread to 4096 columns, four beyond (8192 columns 47 us, by two
+// 53); 768 threads in fewer registers were slower on short batches (4099 x 1000 bf16 13.6 us, 10.8 with 512).
 template <typename TD, typename TH, int N, int NV, bool RING, bool WIDE>
 __global__ void __launch_bounds__(BACKWARD_THREADS) rms_norm_backward_kernel(const __grid_constant__ Grad p) {
   __shared__ Exchange ex;

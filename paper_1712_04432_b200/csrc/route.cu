@@ -12,7 +12,8 @@
 // to one is known by what it lacks, which a float has to 4e-7 of itself, so that keys of the best experts are good to some 1e-8, where their
 // sum as a float would be good to 1e-7.  What that cannot tell apart (unless logits and biases are the same) is settled in
 // double, about one token in ten thousand: it costs a token's warp, and so the whole call, microseconds.  (With keys as floats one token in 300
-// was: 8150 tokens of 256 experts 29 us.)
+// was: 8150 tokens of 256 experts in groups 29 us, now 18.)  Instructions bound large calls, about 1050 a token there; 16 tokens take 3.2 us, the latency
+// of one token and the sums over the experts.
 //
 // Places: a block marks for each expert which of 64 tokens chose it, one bit a token, so a slot's rank is a count of bits and neither
 // it nor anything else depends on the order of atomics.  A second kernel adds up the blocks' counts (up to 64 tokens are one block, and one launch).
@@ -271,7 +272,8 @@ template <int N> __device__ __forceinline__ void sort_falling(uint32_t (&s)[N]) 
 // softmax needs them.
 struct Choice { int id; float z, top, total; bool unsure; };          // z: the logit of expert id
 
-// first_e: the lane's first expert.  list: k words of the warp's in shared memory.  Keys with a bias: fixed if all biases are within 0.99, (score + bias + 1) 2^30, the biases' share in shared memory; else the float sum's code.
+// first_e: the lane's first expert.  list: k words of the warp's in shared memory.  Keys with a bias: fixed if all biases are within 0.99,
+// (score + bias + 1) 2^30, the biases' share in shared memory; else the float sum's code.
 template <int NPL, typename T>
 __device__ __forceinline__ Choice choose(const Route& p, const T* row, const float (&l)[NPL], const float* bias, const uint32_t* bias_steps, bool fixed, uint2* list,
                                         int first_e, int lane) {
@@ -327,6 +329,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
   // part there is, a half or the largest p, whose sum's error counts with it; the steps' rounding and the bits given away.
   const float part = p.sigmoid ? 0.5f : inv_total;
   const float relative = p.sigmoid ? 4e-7f : 2e-6f, coarse = 2.f * relative * part;
+  const float coarse_float = coarse + (p.sigmoid ? 2e-7f : 0.f);              // (one minus the small part is rounded there, too)
   if (p.G > 1) {
     const bool by_score = by_two && !p.bias, sums = by_two && (fixed || by_score);
     // a lane's two best of a group, as the group counts them
@@ -385,7 +388,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
         c.unsure = out <= 2 * NAN_CODE || in - out <= static_cast<uint32_t>(coarse * STEPS) + 2 * NPL + 4;
       else {
         const float a = value_of(in), b = value_of(out);
-        c.unsure = !(a - b > 2.f * coarse + 2.f * (NPL + 2) * 1.2e-7f * fabsf(a));
+        c.unsure = !(a - b > 2.f * coarse_float + 2.f * (NPL + 2) * 1.2e-7f * fabsf(a));
       }
     }
   }
@@ -412,7 +415,7 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
   auto close = [&](uint32_t hi, uint32_t lo) {
     if (!p.bias || fixed) return hi - lo <= reach || lo <= 2 * NAN_CODE;
     const float v = value_of(hi);
-    return !(v - value_of(lo) > coarse + (NPL + 2) * 1.2e-7f * fabsf(v));
+    return !(v - value_of(lo) > coarse_float + (NPL + 2) * 1.2e-7f * fabsf(v));
   };
   const uint32_t next = __shfl_down_sync(0xffffffffu, mine, 1), last = __shfl_sync(0xffffffffu, mine, p.k - 1), left = key[0] & ~LOW;
   const bool near_next = lane + 1 < chosen && close(mine, next), near_left = chosen == p.k && left && close(last, left);
@@ -577,7 +580,8 @@ __global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Rou
 }
 
 // Each block takes the slots of one block of the kernel above: it adds up all blocks' counts, which gives the experts' first rows, and those
-// of the blocks before its own; eight experts a thread, the blocks dealt out to STRANDS threads, all of whose loads are under way at once.
+// of the blocks before its own; eight experts a thread, the blocks dealt out to STRANDS threads, all of whose loads are under way at once.  About 5 us
+// with its launch: four dependent round trips and barriers.
 constexpr int STRANDS = 8;
 __global__ void __launch_bounds__(512) places_kernel(const __grid_constant__ Route p) {
   __shared__ int total[MAX_E + 1], before[MAX_E];
@@ -644,7 +648,7 @@ struct RouteGrad {
 };
 
 // One warp per token; its row of the result is put together in shared memory, the slots' shares one after the other (the same expert
-// named twice gets both).
+// named twice gets both).  16384 x 512 floats of 12 slots: 20 us (3.4 TB/s); 8192 x 64 bf16 5 us, latency.
 constexpr int GRAD_WARPS = 8;
 template <typename T>
 __global__ void __launch_bounds__(32 * GRAD_WARPS) route_backward_kernel(const __grid_constant__ RouteGrad p) {
