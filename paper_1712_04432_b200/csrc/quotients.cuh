@@ -1,6 +1,8 @@
 // Rows in 8 bits: s = max |x| / 127 in float, q = x / s rounded to the nearest integer (halves to even).  The scale of a row and the
 // quotients of eight of its values, shared by the row quantiser and the norm that leaves its rows in 8 bits.
 #pragma once
+#include <stdint.h>
+
 #include "pairs.cuh"
 
 namespace mbd {
