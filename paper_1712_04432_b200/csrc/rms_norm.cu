@@ -25,6 +25,7 @@ struct Norm {
 // h of one vector, from what was loaded; with a residual it is rounded to the residual's type.
 template <typename TX, typename TR, bool RES>
 __device__ __forceinline__ Raw8<TR> stream8(const Raw8<TX>& x, const Raw8<TR>& res) {
+  if constexpr (!RES && sizeof(TX) == sizeof(TR)) return x;
   Raw8<TR> h;
   float v[8];
 #pragma unroll
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(N < 128 ? 128 : N) rms_norm_direct_kernel(cons
 }
 
 // Many rows with little traffic each (no residual, or results in 8 bits): one block per SM, blockDim.x / N rows at a time, which come through
-// shared memory, p.stages rows deep; the gain lies there too.  8192 x 4096 bf16 25 us (5.4 TB/s), in 8 bits 33 us: instructions bound that one.
+// shared memory, p.stages rows deep; the gain lies there too.  8192 x 4096 bf16 24 us (5.5 TB/s), in 8 bits 31 us: instructions bound that one.
 template <typename TX, typename TR, bool RES, int N, int NV>
 __global__ void __launch_bounds__(FORWARD_THREADS) rms_norm_ring_kernel(const __grid_constant__ Norm p) {
   constexpr bool WIDE = true;
@@ -409,7 +410,7 @@ cudaError_t launch_ring(const Norm& p, const Shape& s, int sms, cudaStream_t str
 
 // Few rows go one per block, for the latency.  Others go directly where their traffic hides what a row costs besides (8 bytes a value: 8192 x
 // 4096 bf16 with residual 43 us, by the ring 48; 8192 x 2048 floats with one 42, 48), or where they are too few to fill the ring (2000 x 4096 without
-// a residual 9.4 us, 10.4; 1000 x 1024 with one 2.5, 4.6); through the ring where there is less traffic (8192 x 4096 bf16 without a residual 25 us,
+// a residual 9.4 us, 10.4; 1000 x 1024 with one 2.5, 4.6); through the ring where there is less traffic (8192 x 4096 bf16 without a residual 24 us,
 // directly 32; in 8 bits with one 43, 48).  Rows of more than 8192 values go through the ring if they fit, or else are read twice.
 template <typename TX, typename TR, bool RES, bool WIDE>
 cudaError_t launch_norm(Norm p, int sms, cudaStream_t stream) {
