@@ -514,7 +514,7 @@ MBD_API mbd_status mbd_rms_norm(int64_t R, int64_t K, const void* X_dev, int x_b
  * (h_bf16), dX is the gradient of both x and the residual.  d_gain_dev (float [K], NULL: not asked for) is overwritten; it is summed in a
  * fixed order through scratch_dev (min(R, MBD_NORM_SCRATCH_ROWS) * K floats, contents of no matter; calls in flight at the same time need
  * one each).  dX_dev may be the memory of dY (same type), h or d_residual; otherwise as above. */
-enum { MBD_NORM_SCRATCH_ROWS = 592 };
+enum { MBD_NORM_SCRATCH_ROWS = 160 };
 MBD_API mbd_status mbd_rms_norm_backward(int64_t R, int64_t K, const void* dY_dev, int dy_bf16, int64_t lddy, const void* H_dev, int h_bf16,
                                  int64_t ldh, const float* gain_dev, double eps, const void* d_residual_dev, int64_t lddres, void* dX_dev,
                                  int64_t lddx, float* d_gain_dev, float* scratch_dev, void* cuda_stream);
@@ -555,7 +555,7 @@ MBD_API mbd_status mbd_expert_route_backward(const mbd_router* router_host, int6
 
 /* ---- Rows to the experts and back ----
  * places [T, k] as mbd_expert_route leaves them, `rows` the rows of the tensor sorted by expert; a place outside [0, rows) is an empty
- * slot.  Places are distinct (rows named twice get one of the two).  k <= 32, K any.  All enqueue only and keep no state.
+ * slot.  Places are distinct (a row that is named twice holds values of either token, and nothing outside it is touched).  k <= 32, K any.  All enqueue only and keep no state.
  * dispatch: out[places[t, j], :] = X[t, :], elements of 1, 2 or 4 bytes as they are, and out_scale[places[t, j]] = scale[t] for rows in 8 bits
  *   (both NULL otherwise).  Rows of `out` in no place stay as they are.
  * combine:  out[t, :] = residual[t, :] + sum over the slots of weights[t, j] * Y[places[t, j], :] in float in the order of j, rounded once.  weights NULL: ones

@@ -466,7 +466,7 @@ __device__ __forceinline__ float share(float z, bool there, bool by_sigmoid, boo
   const float most = !by_sigmoid || tiny ? warp_max(there ? z : -CUDART_INF_F) : 0.f;
   const float r = !there || z == -CUDART_INF_F ? 0.f : by_sigmoid && !tiny ? sigmoid(z) : expf(z - most);
   const float sum = warp_sum(r);
-  return there && sum != 0.f ? __fdividef(r, sum) : 0.f;
+  return there && sum != 0.f ? __fdiv_rn(r, sum) : 0.f;       // (the only one chosen: exactly 1, and its gradient exactly 0)
 }
 
 // Exclusive sums of E numbers in shared memory, by a block of at least as many threads; all of them go behind the last.

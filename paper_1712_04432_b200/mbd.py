@@ -88,7 +88,7 @@ class GridRow(C.Structure):
 
 
 ROUTE_SOFTMAX, ROUTE_SIGMOID = range(2)
-NORM_SCRATCH_ROWS = 592
+NORM_SCRATCH_ROWS = 160
 
 
 class Router(C.Structure):

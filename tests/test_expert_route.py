@@ -443,6 +443,20 @@ def test_gradient(T, E, k, score, renormalise):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("score", [0, 1])
+def test_one_expert_renormalised_has_weight_one_and_no_gradient(score):
+    """Exactly: the weight does not depend on the logits."""
+    import torch
+    for dtype in ("f32", "bf16"):
+        r = mbd.Router(70, 1, score, True, scale=2.5)
+        logits, _ = _logits(500, 70, dtype, 3, scale=20.0)
+        ids, w, _, _ = _route(r, logits)
+        assert (w == 2.5).all()
+        dw = torch.randn(500, 1, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+        assert not _backward(r, logits, ids, dw).any()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("score,renormalise", [(0, True), (0, False), (1, True), (1, False)])
 def test_gradient_of_given_ids(score, renormalise):
     """Ids out of range, an expert named twice, masked experts, a row of nothing, far logits."""
