@@ -761,8 +761,9 @@ def rms_norm(x, gain=None, residual=None, h=None, y=None, q=None, scale=None, ep
     assert h is None or (residual is not None and h_bf16 == r_bf16)
     aq, ldq, ascale = None, 0, None
     if q is not None:
-        assert q.dtype == _t.i8 and q.shape == shape and (q.stride(1) == 1 or K == 1)
-        aq, ldq, ascale = _at(q, dev), (q.stride(0) if R > 1 else K), _dense(scale, _t.f32, (R,), dev)
+        ldq, one = q.stride()
+        assert q.dtype is _t.i8 and q.shape == shape and (one == 1 or K == 1) and q.get_device() == dev
+        aq, ldq, ascale = q.data_ptr(), (ldq if R > 1 else K), _dense(scale, _t.f32, (R,), dev)
     _check(lib().mbd_rms_norm(R, K, ax, x_bf16, ldx, ar, r_bf16, ldr, _dense(gain, _t.f32, (K,), dev), eps, ah, ldh, ay, y_bf16, ldy, aq, ldq, ascale,
                               stream), "mbd_rms_norm")
     return y if y is not None else q
