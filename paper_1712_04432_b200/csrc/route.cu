@@ -338,9 +338,9 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
       if (p.best == 1 || !first) return first;
       if (first <= 2 * NAN_CODE || (second && second <= 2 * NAN_CODE)) return NAN_CODE;
       if (sums) return first / 2 + (second ? second / 2 : 1u << 29);             // (both have one in front)
-      return code_of(value_of(first) + (second ? value_of(second) : 0.f));
+      return code_of(0.5f * value_of(first) + (second ? 0.5f * value_of(second) : 0.f));   // (halves: no sum is beyond a float)
     };
-    uint32_t mine;                                             // the score of this lane's group, or of group `lane`
+    uint32_t mine, one = 0, two = 0;                           // the score of this lane's group, or of group `lane`, and the keys it is made of
     bool keep;
     if (p.group_lanes) {                                       // a lane has experts of one group, a group 1, 2, 4 .. lanes
       uint32_t a = counted(key[0]), b = NPL > 1 ? counted(key[NPL > 1 ? 1 : 0]) : 0u;
@@ -349,6 +349,8 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
         b = max(min(a, a2), max(b, b2));
         a = max(a, a2);
       }
+      one = a;
+      two = b;
       mine = group_score(a, b);
       keep = among_best(mine, p.group_lanes - 1, p.G, p.top_groups, lane);
       if (!keep) {
@@ -369,7 +371,11 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
         }
         const uint32_t first = largest(a), owners = __ballot_sync(0xffffffffu, a == first);
         const uint32_t second = largest(lane == __ffs(owners) - 1 ? b : a);
-        if (lane == g) mine = group_score(first, second);
+        if (lane == g) {
+          one = first;
+          two = second;
+          mine = group_score(first, second);
+        }
       }
       keep = among_best(mine, 0, p.G, p.top_groups, lane);
       const unsigned kept = __ballot_sync(0xffffffffu, keep);
@@ -386,9 +392,11 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
       if (!scored) c.unsure = sizeof(T) == 4 && in == out;
       else if (fixed || by_score)                              // (of two: twice as far off, in steps twice as long)
         c.unsure = out <= 2 * NAN_CODE || in - out <= static_cast<uint32_t>(coarse * STEPS) + 2 * NPL + 4;
-      else {
-        const float a = value_of(in), b = value_of(out);
-        c.unsure = !(a - b > 2.f * coarse_float + 2.f * (NPL + 2) * 1.2e-7f * fabsf(a));
+      else {                                                   // each key is off by its own size, which a sum of two may be far below
+        const float a = value_of(one), b = p.best == 2 && two ? value_of(two) : 0.f, score = value_of(mine);
+        float off = 0.5f * coarse_float + (NPL + 2) * 1.2e-7f * (p.best == 2 ? 0.5f * fabsf(a) + 0.5f * fabsf(b) : fabsf(a));
+        if (a == CUDART_INF_F) off = 0.f;                      // (as it is in exact arithmetic)
+        c.unsure = ~largest(keep ? ~code_of(score - off) : 0u) <= largest(keep || !mine ? 0u : code_of(score + off));
       }
     }
   }

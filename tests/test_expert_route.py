@@ -268,6 +268,36 @@ def test_two_best_of_groups_that_floats_cannot_tell_apart():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("level", [4.0, 16.0, 100.0, 1000.0])
+def test_two_best_of_groups_whose_keys_cancel(score, level):
+    """Biases of both signs, one expert of a group near `level` and the others near -level: sums of two keys next to zero that differ by less than
+    a float has at `level`."""
+    import torch
+    rng = np.random.default_rng(int(level) + score)
+    for E, k, G, top in ((256, 8, 8, 4), (64, 3, 4, 2), (96, 2, 3, 1), (512, 8, 16, 5), (510, 6, 17, 6)):
+        S, part = E // G, 1.0 if score else 1.0 / G
+        first = np.arange(G) * S + rng.integers(0, S // 2, G)
+        second = np.arange(G) * S + rng.integers(S // 2, S, G)
+        bias = (-level - 2 - rng.random(E)).astype(np.float32)
+        bias[first] = level + 0.1 * part * rng.random(G)
+        bias[second] = -level - 0.1 * part * rng.random(G)
+        both = bias[first].astype(np.float64) + bias[second]
+        rows = []
+        for _ in range(40):
+            pa = part * rng.uniform(0.3, 0.4, G)
+            pb = 0.8 * part - both - pa + 3e-8 * level * rng.normal(size=G)
+            if score:
+                l = rng.normal(size=E)
+                l[first], l[second] = np.log(pa / (1 - pa)), np.log(pb / (1 - pb))
+            else:
+                l = np.full(E, np.log((1 - pa.sum() - pb.sum()) / (E - 2 * G)))
+                l[first], l[second] = np.log(pa), np.log(pb)
+            rows.append(l)
+        _compare(mbd.Router(E, k, score, True, G, top, 2), torch.from_numpy(np.array(rows, np.float32)).cuda(), torch.from_numpy(bias).cuda())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("score,renormalise,G", [(0, True, 1), (0, False, 1), (1, True, 1), (1, False, 4), (0, True, 4)])
 def test_equal_keys_masks_and_numbers_that_are_none(score, renormalise, G):
     import torch
