@@ -324,6 +324,18 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
 #pragma unroll
     for (int i = 0; i < NPL; ++i) key[i] = l[i] != -CUDART_INF_F ? (code_of(l[i]) & ~LOW) | (LOW - i) : 0u;
   }
+  // A lane's two best by all of their bits, where a group counts by their scores: the keys cannot tell logits up to NPL - 1 units apart, which
+  // are 1e-4 of a score at logits of 100.
+  const bool by_score = by_two && !p.bias;
+  uint32_t best_a = 0, best_b = 0;
+  if (by_score && p.group_lanes) {
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) {
+      const uint32_t v = l[i] != -CUDART_INF_F ? code_of(l[i]) : 0u;
+      best_b = max(best_b, min(best_a, v));
+      best_a = max(best_a, v);
+    }
+  }
   sort_falling(key);
   // How far the gap between two keys can be off, in steps or (keys that are sums of floats) by value.  Of a score: 4e-7 of the largest small
   // part there is, a half or the largest p, whose sum's error counts with it; the steps' rounding and the bits given away.
@@ -331,8 +343,8 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
   const float relative = p.sigmoid ? 4e-7f : 2e-6f, coarse = 2.f * relative * part;
   const float coarse_float = coarse + (p.sigmoid ? 2e-7f : 0.f);              // (one minus the small part is rounded there, too)
   if (p.G > 1) {
-    const bool by_score = by_two && !p.bias, sums = by_two && (fixed || by_score);
-    // a lane's two best of a group, as the group counts them
+    const bool sums = by_two && (fixed || by_score);
+    // a key as a group counts it
     auto counted = [&](uint32_t k) { return by_score && k ? steps(logit(row, first_e + static_cast<int>(LOW - (k & LOW))), p.sigmoid) : k & ~LOW; };
     auto group_score = [&](uint32_t first, uint32_t second) {
       if (p.best == 1 || !first) return first;
@@ -343,7 +355,12 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
     uint32_t mine, one = 0, two = 0;                           // the score of this lane's group, or of group `lane`, and the keys it is made of
     bool keep;
     if (p.group_lanes) {                                       // a lane has experts of one group, a group 1, 2, 4 .. lanes
-      uint32_t a = counted(key[0]), b = NPL > 1 ? counted(key[NPL > 1 ? 1 : 0]) : 0u;
+      uint32_t a = key[0] & ~LOW, b = NPL > 1 ? key[NPL > 1 ? 1 : 0] & ~LOW : 0u;
+      if (by_score) {
+        a = best_a ? steps(value_of(best_a), p.sigmoid) : 0u;
+        b = best_b ? steps(value_of(best_b), p.sigmoid) : 0u;
+        order(a, b);                                           // (two scores next to each other may be off by a step)
+      }
       for (int d = 1; d < 1 << (p.group_lanes - 1); d *= 2) {
         const uint32_t a2 = __shfl_xor_sync(0xffffffffu, a, d), b2 = __shfl_xor_sync(0xffffffffu, b, d);
         b = max(min(a, a2), max(b, b2));

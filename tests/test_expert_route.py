@@ -298,6 +298,34 @@ def test_two_best_of_groups_whose_keys_cancel(score, level):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("level", [0.5, 10.0, 100.0, -100.0, 1000.0])
+def test_two_best_of_groups_among_logits_a_few_bits_apart(score, level):
+    """Without a bias: the best experts of each group up to 15 units of a float apart, next to each other and far from each other in the group; the
+    differences reach the scores where the logits have a common offset."""
+    import torch
+    rng = np.random.default_rng(int(abs(level)) + score)
+    unit = np.spacing(np.float32(level) * np.float32(0.99))
+    for E, k, G, top in ((256, 8, 8, 4), (512, 8, 8, 1), (512, 6, 16, 3), (128, 4, 8, 2), (64, 4, 4, 2), (160, 5, 5, 2), (510, 6, 3, 1)):
+        S = E // G
+        l = np.full((40, E), level - 20.0, np.float64)
+        for t in range(40):
+            for g in range(G):
+                near = g * S + rng.integers(0, S - 4) + np.arange(4)            # neighbours
+                far = g * S + rng.choice(S, 2, replace=False)
+                for e in (*near, *far):
+                    l[t, e] = level + unit * rng.integers(-15, 1)
+        l = l.astype(np.float32)
+        # Groups whose sums doubles do not tell apart are nobody's to order: a + b units over two experts give the same sum but for s'' u^2 (a^2 - b^2) / 2,
+        # at 0.5 (u = 2^-25, s'' = 0.058, a^2 - b^2 <= 225) 6e-15 and mostly below 1e-16, where a double of two sums with three roundings
+        # of 2^-53 each has 7e-16 < 2^-50 of itself.  Such tokens are left out, but not those whose scores are one in doubles, too: equal keys.
+        sums = np.sort(np.sort(_scores(l, score).reshape(40, G, S), 2)[:, :, -2:].sum(2), 1)
+        l = l[(sums[:, -top] - sums[:, -top - 1] >= 2.0 ** -50 * sums[:, -top]) | (sums[:, -top - 1] == 2.0)]
+        assert len(l) > 10
+        _compare(mbd.Router(E, k, score, True, G, top, 2), torch.from_numpy(l).cuda())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("score,renormalise,G", [(0, True, 1), (0, False, 1), (1, True, 1), (1, False, 4), (0, True, 4)])
 def test_equal_keys_masks_and_numbers_that_are_none(score, renormalise, G):
     import torch
