@@ -484,12 +484,14 @@ __device__ __forceinline__ Choice choose(const Route& p, const T* row, const flo
 }
 
 // The weight of lane j's expert, of logit z; total: over all experts.  Renormalised scores are taken relative to the largest
-// chosen one, so that scores below float's range keep their ratios: sigmoid(z) is exp(z) far below zero.
+// chosen one, so that scores below float's range keep their ratios: a softmax always, sigmoids where one of them is next to the end of the range
+// (exp(-87)) and none is a half or more (the quotients are as small as the scores then); sigmoid(z) exp(-most) = exp(z - most) / (1 + exp(z)).
 __device__ __forceinline__ float share(float z, bool there, bool by_sigmoid, bool renorm, float top, float total) {
   if (!renorm) return there ? (by_sigmoid ? sigmoid(z) : __fdividef(expf(z - top), total)) : 0.f;
-  const bool tiny = by_sigmoid && !__any_sync(0xffffffffu, there && z >= -60.f);
+  const bool tiny = by_sigmoid && __any_sync(0xffffffffu, there && z < -80.f) && !__any_sync(0xffffffffu, there && z >= 0.f);
   const float most = !by_sigmoid || tiny ? warp_max(there ? z : -CUDART_INF_F) : 0.f;
-  const float r = !there || z == -CUDART_INF_F ? 0.f : by_sigmoid && !tiny ? sigmoid(z) : expf(z - most);
+  float r = !there || z == -CUDART_INF_F ? 0.f : by_sigmoid && !tiny ? sigmoid(z) : expf(z - most);
+  if (tiny) r = __fdividef(r, 1.f + expf(z));
   const float sum = warp_sum(r);
   return there && sum != 0.f ? __fdiv_rn(r, sum) : 0.f;       // (the only one chosen: exactly 1, and its gradient exactly 0)
 }

@@ -326,6 +326,25 @@ def test_two_best_of_groups_among_logits_a_few_bits_apart(score, level):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("top", [-1e-3, -1.0, -30.0, -59.0, -61.0, -85.0, 0.0, 5.0])
+def test_renormalised_sigmoids_on_both_sides_of_the_smallest_float(top):
+    """Chosen scores that are numbers of full precision beside scores that are not (below e^-87): their quotients are, and so are the gradients."""
+    import torch
+    E, k, T = 32, 6, 30
+    rng = np.random.default_rng(int(abs(top)))
+    l = np.full((T, E), -400.0, np.float32)
+    for t in range(T):
+        at = rng.permutation(E)[:k]
+        l[t, at] = np.concatenate([[top], rng.uniform(-104.0, min(top, -70.0), k - 1)])
+    r = mbd.Router(E, k, 1, True)
+    logits = torch.from_numpy(l).cuda()
+    got = _compare(r, logits)
+    dw = torch.randn(T, k, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    ids = torch.from_numpy(got[0]).cuda()
+    _close(_backward(r, logits, ids, dw), l, got[0], dw.cpu().numpy(), r)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("score,renormalise,G", [(0, True, 1), (0, False, 1), (1, True, 1), (1, False, 4), (0, True, 4)])
 def test_equal_keys_masks_and_numbers_that_are_none(score, renormalise, G):
     import torch
