@@ -330,3 +330,89 @@ def test_captured_and_replayed():
     g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, (h, y, dx, dg)))
+
+
+# ---------------------------------------------------------------------------------------------------- the forms of large batches
+# More than 10 million values, or 2 rows for each of 148 SMs: rows in whole vectors through shared memory, several a block, each many times
+# around its stages; the row of each width's end and one a vector shorter.
+RING = [(24000, 512), (24000, 504), (24000, 1024), (24000, 1016), (12000, 2048), (12000, 2040), (6000, 4096), (6000, 4088), (3000, 8192), (3000, 8184),
+        (1500, 16384), (1500, 16376)]
+
+
+def _quotients(u):
+    """scale and q of float rows, from the definition: a quotient in 64 bits is that of two floats on the right side of every half step."""
+    import torch
+    s = (u.abs().amax(1).double() / 127).float()                     # (24 bits by 7: 2^-32 from a half step at least)
+    return s, torch.round(u.double() / s.double()[:, None]).clamp(-127, 127).to(torch.int8)
+
+
+def _run_large(R, K, x, res, out, eight, in_place=False):
+    import torch
+    gen = _gen(R + K)
+    randn = lambda *s: torch.randn(*s, device="cuda", generator=gen)  # noqa: E731
+    X = (randn(R, K) * torch.exp(randn(R, 1))).to(_type(x))
+    residual = (randn(R, K) * 2).to(_type(res)) if res != "none" else None
+    g = 1 + 0.3 * randn(K)
+    held = X.clone() if residual is None else (X.float() + residual.float()).to(residual.dtype)
+    h = (residual if in_place else torch.full_like(residual, 5.0)) if residual is not None else None
+    y = (X if in_place else torch.full((R, K), 5.0, dtype=_type(out), device="cuda")) if out != "none" else None
+    q, s = (torch.full((R, K), 99, dtype=torch.int8, device="cuda"), torch.full((R,), -1.0, device="cuda")) if eight else (None, None)
+    mbd.rms_norm(X, gain=g, residual=residual, h=h, y=y, q=q, scale=s, eps=EPS)
+    if h is not None:
+        assert torch.equal(h, held)
+    want, r = _norm64(held, g)
+    rel = (_n(K) / 2 + 8) * U
+    if y is not None:
+        _check(y, want, want.abs(), rel, y.dtype)
+    if eight:
+        ws, wq = _quotients(held.float() * g)
+        assert torch.equal(q, wq)
+        ws = ws.double() * r[:, 0]
+        _check(s, ws, ws, rel, torch.float32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R,K", RING)
+@pytest.mark.parametrize("x,res,out,eight", [("bf16", "none", "bf16", False), ("f32", "none", "bf16", False), ("bf16", "none", "none", True), ("f32", "none", "f32", True),
+                                             ("bf16", "bf16", "bf16", True)])
+def test_forward_of_large_batches_through_shared_memory(R, K, x, res, out, eight):
+    _run_large(R, K, x, res, out, eight)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R,K", RING[::2])
+def test_forward_of_large_batches_in_place(R, K):
+    _run_large(R, K, "bf16", "none", "bf16", False, in_place=True)
+    _run_large(R, K, "bf16", "bf16", "bf16", True, in_place=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R,K", [(2500, 4096), (700, 4088), (600, 2056), (501, 3001), (2500, 8192), (900, 8184), (300, 4097), (9001, 1024), (20000, 504), (2000, 4000), (401, 511), (401, 1021)])
+@pytest.mark.parametrize("x,res,out", [("bf16", "bf16", "bf16"), ("f32", "f32", "f32"), ("bf16", "f32", "bf16"), ("f32", "bf16", "f32"), ("bf16", "none", "bf16"),
+                                       ("f32", "none", "f32")])
+def test_forward_of_large_batches_row_by_row(R, K, x, res, out):
+    _run_large(R, K, x, res, out, False)
+    if x == "bf16":
+        _run_large(R, K, x, res, out, False, in_place=x == out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R,K", [(24000, 512), (24000, 504), (12000, 1024), (12000, 1016), (6000, 2048), (6000, 2040), (3000, 4096), (3000, 4088), (1500, 8192),
+                                 (1500, 8184), (700, 16384), (700, 16376), (6000, 511), (5003, 1001), (3001, 2047), (1501, 4001), (1001, 8191), (450, 16383)])
+@pytest.mark.parametrize("dy,h,dres", [("bf16", "bf16", True), ("bf16", "bf16", False), ("f32", "f32", False), ("f32", "f32", True), ("bf16", "f32", True), ("f32", "bf16", False)])
+def test_backward_of_large_batches(R, K, dy, h, dres):
+    """A block's row groups take many rows each.  dx: n / 2 + 2 roundings of r in three places, n of the dot product, eight of the products, sums and 1 / K.  d_gain: at most R / 148 rows one after the other in a group or, where a block has several groups, fewer
+    and one step for each of at most 16 groups, then five blocks one after the other in each of 32 strands and five steps between those."""
+    import torch
+    gen = _gen(3 * R + K)
+    randn = lambda *s: torch.randn(*s, device="cuda", generator=gen)  # noqa: E731
+    H, D, g = (randn(R, K) * torch.exp(randn(R, 1))).to(_type(h)), (randn(R, K) * 0.1).to(_type(dy)), 1 + 0.3 * randn(K)
+    res = (randn(R, K) * 0.1).to(H.dtype) if dres else None
+    dx, dg = torch.full_like(H, 5.0), torch.full((K,), 5.0, device="cuda")
+    mbd.rms_norm_backward(D, H, dx, gain=g, d_residual=res, d_gain=dg, eps=EPS)
+    want, mag, wg, magg = _backward64(D, H, g, res)
+    _check(dx, want, mag, (2.5 * _n(K) + 14) * U, dx.dtype)
+    _check(dg, wg, magg, (-(-R // 148) + 16 + 10 + _n(K) / 2 + 8) * U, torch.float32)
+    again = torch.empty_like(dg)
+    mbd.rms_norm_backward(D, H, H if res is None else res, gain=g, d_residual=res, d_gain=again, eps=EPS)      # in place: the same bits
+    assert torch.equal(H if res is None else res, dx) and torch.equal(again, dg)
