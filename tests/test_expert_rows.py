@@ -253,3 +253,53 @@ def test_rows_behind_2_to_the_31_elements():
     dw = torch.empty(3, 2, device="cuda")
     mbd.expert_combine_backward(x, Y, places, w, Y, dw)
     assert torch.equal(Y[rows - 1], (x[0].float() * w[0, 0]).to(torch.bfloat16))
+
+
+# ---------------------------------------------------------------------------------------------------- the forms of large batches
+# From 512 tokens and 512 columns on a thread has two or four vectors; the last one ragged, more columns than a block's threads have at once, and
+# rows that move element by element.
+LARGE = [(513, 1, 512), (513, 2, 4096), (600, 1, 1032), (520, 2, 520), (520, 3, 520), (515, 4, 1000), (513, 3, 4104), (514, 5, 1024), (515, 8, 1024), (513, 7, 4104),
+         (512, 2, 16392), (512, 4, 9000), (512, 6, 9000), (513, 32, 520), (530, 2, 1001), (512, 5, 2049)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,k,K", LARGE)
+@pytest.mark.parametrize("y,out", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
+def test_combine_of_large_batches(T, k, K, y, out):
+    test_combine(T, k, K, y, out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,k,K", LARGE)
+@pytest.mark.parametrize("d,y", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
+def test_combine_backward_of_large_batches(T, k, K, d, y):
+    test_combine_backward(T, k, K, d, y)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,k,K", LARGE)
+@pytest.mark.parametrize("dtype", ["bf16", "f32", "i8"])
+def test_dispatch_of_large_batches(T, k, K, dtype):
+    test_dispatch(T, k, K, dtype)
+
+
+@pytest.mark.gpu
+def test_products_with_rows_behind_2_to_the_31_elements():
+    """d_weights of rows at both ends of a tensor of 2.17e9 elements: eight products a thread, the steps within a warp and between the warps."""
+    import torch
+    rows, K = 530000, 4104
+    Y = torch.empty(rows, K, dtype=torch.bfloat16, device="cuda")
+    gen = _gen(6)
+    places = torch.tensor([[rows - 1, 0], [rows - 2, 5], [rows - 9, -1]], dtype=torch.int32, device="cuda")
+    for at in places.flatten().tolist():
+        if at >= 0:
+            Y[at] = _normal(gen, K, dtype="bf16")
+    x, w, dw = _normal(gen, 3, K, dtype="bf16"), _normal(gen, 3, 2), torch.full((3, 2), 5.0, device="cuda")
+    picked = torch.stack([torch.stack([Y[max(at, 0)] for at in row]) for row in places.tolist()]).double()
+    mbd.expert_combine_backward(x, Y, places, w, Y, dw)
+    prod = x.double()[:, None] * picked * (places >= 0).unsqueeze(2)
+    _check(dw, prod.sum(2), prod.abs().sum(2), (24 + K / 256) * U)
+    for t in range(3):
+        for j in range(2):
+            if int(places[t, j]) >= 0:
+                assert torch.equal(Y[int(places[t, j])], (x[t].float() * w[t, j]).bfloat16())
