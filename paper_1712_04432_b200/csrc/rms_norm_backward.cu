@@ -358,8 +358,11 @@ cudaError_t launch_rows(const Grad& p, const Shape& s, int64_t grid, cudaStream_
     case 2 * 1024 + 128: return launch_shape<rms_norm_backward_kernel<TD, TH, 128, 2, RING, WIDE>>(p, s, bytes, grid, stream);
     case 2 * 1024 + 256: return launch_shape<rms_norm_backward_kernel<TD, TH, 256, 2, RING, WIDE>>(p, s, bytes, grid, stream);
     case 4 * 1024 + 256: return launch_shape<rms_norm_backward_kernel<TD, TH, 256, 4, RING, WIDE>>(p, s, bytes, grid, stream);
-    default: return launch_shape<rms_norm_backward_kernel<TD, TH, 512, 4, RING, WIDE>>(p, s, bytes, grid, stream);
+    default: break;
   }
+  if constexpr (!RING || sizeof(TD) + sizeof(TH) == 4)        // (two stages of such rows with floats among them are more than a block has)
+    return launch_shape<rms_norm_backward_kernel<TD, TH, 512, 4, RING, WIDE>>(p, s, bytes, grid, stream);
+  return cudaErrorInvalidValue;
 }
 
 template <typename TD, typename TH, bool WIDE>

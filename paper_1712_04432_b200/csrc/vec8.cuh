@@ -111,19 +111,6 @@ __device__ __forceinline__ void store8(float* row, int t, int j, int n, int K, c
     }
   }
 }
-// Floats to a row of either type.
-template <bool WIDE>
-__device__ __forceinline__ void store8(void* base, int bf16, int64_t row_start, int t, int j, int n, int K, const float* v) {
-  if (bf16) {
-    Raw8<__nv_bfloat16> r;
-    r.set(v);
-    store8<WIDE>(static_cast<__nv_bfloat16*>(base) + row_start, t, j, n, K, r);
-  } else {
-    Raw8<float> r;
-    r.set(v);
-    store8<WIDE>(static_cast<float*>(base) + row_start, t, j, n, K, r);
-  }
-}
 
 // ---- host: where a tensor of rows lies ------------------------------------------------------------------------------
 struct Rows {
