@@ -524,13 +524,14 @@ MBD_API mbd_status mbd_rms_norm_backward(int64_t R, int64_t K, const void* dY_de
  * expert that the products grouped by expert want:
  *     p = softmax(logits) or sigmoid(logits);   key = p + bias (bias_dev float [E], for balance: it has no part in the weights; NULL: none)
  *     groups > 1: the experts are `groups` equal runs; a run's score is its largest key (group_best = 1) or the sum of its two
- *         largest (2); the experts outside the top_groups best runs are out
+ *         largest (2; the largest alone where only one of the run has a key above -inf); the experts outside the top_groups best runs are out
  *     ids[t, j]     the expert with the j-th largest key; equal keys by rising index (of runs, too)
  *     weights[t, j] scale * p, or scale * p / (sum of the chosen p) with renormalise (a softmax then needs the chosen logits only)
  *     places[t, j]  the row of slot (t, j) when all slots are sorted by expert, those of one expert by rising t;
  *     offsets[e]    the first row of expert e, offsets[E] the number of rows: what mbd_expert_gemm_* read
  * The choice is that of the formulas in exact arithmetic but for differences below a double's: keys that floats cannot tell apart are computed again
- * in double.  An expert whose logit or key is -inf is never chosen; where fewer than k are left the last slots are empty: id -1, weight 0, place -1, no
+ * in double.  That takes time (8192 tokens of 256 experts in runs: 18 us, 30 where a token's runs are, 75 where every token's are, as with logits that are
+ * all equal).  An expert whose logit or key is -inf is never chosen; where fewer than k are left the last slots are empty: id -1, weight 0, place -1, no
  * row.  A NaN key comes after all numbers; its weight is NaN.  count_dev (one int32 on the device, NULL: all): only the first
  * min(max(count, 0), T) tokens are routed, the slots of the others are empty: a padded batch, in a captured graph too.
  * ids, weights, places: dense [T, k]; offsets [E + 1].  scratch_dev: mbd_expert_route_scratch(T, E) int32, 16-byte aligned (0 for up to 64 tokens: NULL), contents

@@ -11,9 +11,11 @@
 // it, and that lane's list moving up.  Logits become integers of the same order.  Scores plus biases are counted in steps of 2^-30: a score next
 // to one is known by what it lacks, which a float has to 4e-7 of itself, so that keys of the best experts are good to some 1e-8, where their
 // sum as a float would be good to 1e-7.  What that cannot tell apart (unless logits and biases are the same) is settled in
-// double, about one token in ten thousand: it costs a token's warp, and so the whole call, microseconds.  (With keys as floats one token in 300
-// was: 8150 tokens of 256 experts in groups 29 us, now 18.)  Instructions bound large calls, about 1050 a token there; 16 tokens take 3.2 us, the latency
-// of one token and the sums over the experts.
+// double, about one token in ten thousand: it costs a token's warp, and so the whole call, microseconds.  8150 tokens of 256 experts in groups, biases of
+// 0.05: 17.5 us in nine of ten sets of inputs, 30 in the one with a token whose groups were settled so.  Keys are floats where a bias is beyond 0.99: one
+// token in 300 is settled, 31 us.  Groups that tie are always settled: 66 us with logits and biases of zero, 75 without biases.  Without groups 14 us,
+// 45 with equal logits (the list of what ties with the last choice is gone through).  Instructions bound large calls, about 1050 a token with groups; 16
+// tokens take 3.3 us, the latency of one token and the sums over the experts.
 //
 // Places: a block marks for each expert which of 64 tokens chose it, one bit a token, so a slot's rank is a count of bits and neither
 // it nor anything else depends on the order of atomics.  A second kernel adds up the blocks' counts (up to 64 tokens are one block, and one launch).
@@ -553,7 +555,7 @@ __global__ void __launch_bounds__(1024) route_kernel(const __grid_constant__ Rou
     for (int e = threadIdx.x; e < p.E * (SUB / 32); e += blockDim.x) chose[0][e] = 0u;
     __syncthreads();
     const int tokens = static_cast<int>(min(end - sub, static_cast<int64_t>(SUB)));
-    constexpr bool AHEAD = NPL < 16;                           // (with 16 more registers a thread 512 threads fit, not 1024: 16384 tokens of 512 experts 107 instead of 99 us)
+    constexpr bool AHEAD = NPL < 16;                           // (with 16 more registers a thread 512 threads fit, not 1024: 16384 tokens of 512 experts took 107 instead of 99 us)
     float next[NPL];                                           // the warp's next token is on its way
     if (AHEAD && warp < tokens) logits_of<NPL>(static_cast<const T*>(p.logits) + (sub + warp) * p.ld, first_e, count, p.whole, next);
     for (int i = warp; i < tokens; i += warps) {
